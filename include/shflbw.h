@@ -259,11 +259,117 @@ int shflbw_layernorm_transpose(const void* x, int64_t ldx, const void* gamma, co
                                float eps, int normalize, void* out, int64_t ldo, int64_t N,
                                int K, shflbw_dtype dtype, void* stream);
 
+/*
+ * Cache of keys and values in 4 bits, in pages, for serving.  Activations are
+ * features x tokens with the tokens innermost, as shflbw_spmm takes and leaves
+ * them; head h owns rows h * head_dim and up.
+ *
+ * Format: 32 features of one token and head share a scale 2^e, e =
+ * floor(log2(largest magnitude)) - 2, at least -126; a value is a sign and one
+ * of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times the scale, the nearest, ties to the code
+ * with an even last bit, what is beyond 6 to 6.  A block that holds an
+ * infinity or a NaN is stored as NaN as a whole.
+ *
+ *  data         device, caller-owned, shflbw_kv_cache_bytes bytes, 128-byte
+ *               aligned.  Slots that were never written hold what was there.
+ *  pages, page_tokens  page_tokens is a power of two from 32 to 1024, pages *
+ *               page_tokens below 2^31.  Slot = page * page_tokens + place in
+ *               the page.
+ *  heads, head_dim  heads of keys (and of values); head_dim 64, 96 or 128.
+ *  dtype        SHFLBW_F16 or SHFLBW_BF16: of everything that goes in or out.
+ */
+typedef struct {
+    void* data;
+    int32_t pages, page_tokens, heads, head_dim, dtype;
+} shflbw_kv_cache;
+
+/* Bytes of device memory of such a cache; 0 where the sizes are not supported. */
+size_t shflbw_kv_cache_bytes(int pages, int page_tokens, int heads, int head_dim);
+
+/* Quantises column t of k and v (device, heads * head_dim x tokens, leading
+ * dimensions ldk, ldv >= tokens) into slot slots[t] (device), for every t.  A
+ * slot that is negative or beyond the cache is skipped.  Two columns with one slot:
+ * either may be stored, in parts.  Enqueues on `stream` only. */
+int shflbw_kv_write(const shflbw_kv_cache* cache, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                    const int32_t* slots, int64_t tokens, void* stream);
+
+/* The reverse: column t of k and v becomes what slot slots[t] holds, rounded to
+ * dtype (exact but for binary16 below 2^-21); NaN for slots outside the cache. */
+int shflbw_kv_read(const shflbw_kv_cache* cache, const int32_t* slots, int64_t tokens, void* k, int64_t ldk,
+                   void* v, int64_t ldv, void* stream);
+
+/*
+ * The sequences of a shflbw_kv_attention call.  Query head i attends with key
+ * head i / (q_heads / heads).  A sequence's queries are its last tokens, whose
+ * keys and values the cache already holds: with n queries and length L, query
+ * i stands at position L - n + i, and sees the key at position j if j is not
+ * past it and (no window, or it lies less than `window` back, or j < sinks).
+ *  tokens       columns of q in all
+ *  table        device, batch x table_pages pages (leading dimension table_ld):
+ *               sequence b's token j lies in page table[b][j / page_tokens].  Entries past a
+ *               sequence's length are not looked at; a page that is not in the cache reads as NaN.
+ *  lengths      device, batch: cached tokens of every sequence, the new ones
+ *               among them.  0: its queries see nothing and get zeros.  Beyond
+ *               table_pages pages: NaN.
+ *  starts       device, batch + 1: sequence b's queries are columns starts[b] to
+ *               starts[b + 1] - 1, in order.  NULL: one each, column b (tokens ==
+ *               batch, max_queries == 1).  Columns of no sequence are left undefined.
+ *  max_queries, max_length  at least what any sequence has: queries past the
+ *               former are left undefined; the latter decides how the work is
+ *               cut, never what is computed.
+ *  window       0: none
+ * The struct is host memory; what it points to is device memory.
+ */
+typedef struct {
+    int32_t q_heads, batch, max_queries, table_pages, window, sinks;
+    int64_t tokens, max_length, table_ld;
+    const int32_t *table, *lengths, *starts;
+} shflbw_kv_sequences;
+
+/* Bytes of device workspace that shflbw_kv_attention needs (may be 0; the
+ * pointers of the structs are not followed), or a negative status. */
+int64_t shflbw_kv_attention_workspace(const shflbw_kv_cache* cache, const shflbw_kv_sequences* sequences);
+
+/*
+ * Attention over the cache: out = softmax(q k / sqrt(head_dim)) v per query
+ * head, over the keys a query sees, one token or many per sequence.
+ *  q, out  device, q_heads * head_dim x tokens of the cache's dtype, leading
+ *          dimensions ldq, ldo >= tokens.  out must not overlap q.
+ *  workspace  device, 16-byte aligned, at least shflbw_kv_attention_workspace bytes; its
+ *          contents are free again when the call's work has ended.  NULL where 0 bytes are needed.
+ * Scores, softmax and sums are in binary32, weights are rounded to dtype for
+ * their product with the values.  Keys and values that a query does not see
+ * never reach its result, whatever they hold.  Two calls with the same
+ * arguments give the same bits.  Enqueues on `stream` only.
+ */
+int shflbw_kv_attention(const shflbw_kv_cache* cache, const shflbw_kv_sequences* sequences, const void* q, int64_t ldq,
+                        void* out, int64_t ldo, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Attention of prompts to themselves, causal, with an optional sliding window
+ * and first tokens (sinks) that stay visible; keys and values in 16 bits.
+ *  q, out  device, q_heads * head_dim x tokens of dtype; k, v: heads * head_dim
+ *          x tokens; tokens innermost, leading dimensions >= tokens.  out must
+ *          not overlap the others.
+ *  starts  device, sequences + 1: sequence b is columns starts[b] to starts[b + 1] - 1
+ *          (it may be empty).  NULL: one sequence of all columns.  Columns of no sequence
+ *          are left undefined.
+ *  max_tokens  at least the longest sequence's; tokens past it are left undefined.
+ *  window  the key at j is visible from p if j <= p and (window 0, or p - j <
+ *          window, or j < sinks)
+ * Accuracy, hidden keys and values, and determinism as in shflbw_kv_attention.
+ * Any alignment and leading dimension.  Enqueues on `stream` only.
+ */
+int shflbw_window_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                            void* out, int64_t ldo, int q_heads, int heads, int head_dim, int64_t tokens,
+                            const int32_t* starts, int sequences, int64_t max_tokens, int window, int sinks,
+                            shflbw_dtype dtype, void* stream);
+
 const char* shflbw_status_string(int status);
 const char* shflbw_last_error(void); /* thread-local, never NULL */
 
-/* Which kernel the calling thread's most recent successful shflbw_spmm or shflbw_conv2d
- * launched, as "name<template arguments>" (the automatic choice of set_tuning(0, 0) is
+/* Which kernel the calling thread's most recent successful shflbw_spmm, shflbw_conv2d,
+ * shflbw_kv_attention or shflbw_window_attention launched, as "name<template arguments>" (the automatic choice of set_tuning(0, 0) is
  * made per call from the matrix and the operand shape).  Thread-local, never NULL; empty
  * before the first launch. */
 const char* shflbw_last_kernel(void);

@@ -7,6 +7,7 @@ stream handle; numpy arrays for host-side inputs of the compressor.
 The library is required: if ``libshflbw.so`` has not been built this module
 raises at first use.  There is no CPU fallback.
 """
+import contextlib
 import ctypes
 import os
 
@@ -26,7 +27,8 @@ EXPORTS = [
     "shflbw_group_columns", "shflbw_decompress", "shflbw_device_bytes", "shflbw_bind_device",
     "shflbw_set_tuning", "shflbw_device_status", "shflbw_set_wait_limit", "shflbw_spmm", "shflbw_spmm_unbound",
     "shflbw_conv2d",
-    "shflbw_layernorm_transpose", "shflbw_status_string", "shflbw_last_error", "shflbw_last_kernel",
+    "shflbw_layernorm_transpose", "shflbw_kv_cache_bytes", "shflbw_kv_write", "shflbw_kv_read",
+    "shflbw_kv_attention_workspace", "shflbw_kv_attention", "shflbw_window_attention", "shflbw_status_string", "shflbw_last_error", "shflbw_last_kernel",
 ]
 
 
@@ -34,6 +36,17 @@ class ShflbwError(RuntimeError):
     def __init__(self, status, text):
         super().__init__("shflbw status %d (%s): %s" % (status, status_string(status), text))
         self.status = status
+
+
+class _Cache(ctypes.Structure):   # shflbw_kv_cache
+    _fields_ = [("data", ctypes.c_void_p)] + [(name, ctypes.c_int32) for name in
+                                              ("pages", "page_tokens", "heads", "head_dim", "dtype")]
+
+
+class _Sequences(ctypes.Structure):   # shflbw_kv_sequences
+    _fields_ = [(name, ctypes.c_int32) for name in ("q_heads", "batch", "max_queries", "table_pages", "window", "sinks")] + \
+               [(name, ctypes.c_int64) for name in ("tokens", "max_length", "table_ld")] + \
+               [(name, ctypes.c_void_p) for name in ("table", "lengths", "starts")]
 
 
 def lib():
@@ -79,6 +92,19 @@ def lib():
         L.shflbw_layernorm_transpose.restype = i32
         L.shflbw_layernorm_transpose.argtypes = [vp, i64, vp, vp, ctypes.c_float, i32, vp, i64, i64,
                                                  i32, i32, vp]
+        L.shflbw_kv_cache_bytes.restype = ctypes.c_size_t
+        L.shflbw_kv_cache_bytes.argtypes = [i32] * 4
+        cache, sequences = ctypes.POINTER(_Cache), ctypes.POINTER(_Sequences)
+        L.shflbw_kv_write.restype = i32
+        L.shflbw_kv_write.argtypes = [cache, vp, i64, vp, i64, vp, i64, vp]
+        L.shflbw_kv_read.restype = i32
+        L.shflbw_kv_read.argtypes = [cache, vp, i64, vp, i64, vp, i64, vp]
+        L.shflbw_kv_attention_workspace.restype = i64
+        L.shflbw_kv_attention_workspace.argtypes = [cache, sequences]
+        L.shflbw_kv_attention.restype = i32
+        L.shflbw_kv_attention.argtypes = [cache, sequences, vp, i64, vp, i64, vp, i64, vp]
+        L.shflbw_window_attention.restype = i32
+        L.shflbw_window_attention.argtypes = [vp, i64] * 4 + [i32, i32, i32, i64, vp, i32, i64, i32, i32, i32, vp]
         L.shflbw_status_string.restype = ctypes.c_char_p
         L.shflbw_status_string.argtypes = [i32]
         L.shflbw_last_error.restype = ctypes.c_char_p
@@ -391,6 +417,161 @@ def layernorm_transpose(x, gamma=None, beta=None, eps=1e-5, normalize=True, out=
                                             out.stride(0) if K > 1 else N, N, K,
                                             BF16 if x.dtype == torch.bfloat16 else F16,
                                             _stream_ptr(stream)))
+    return out
+
+
+def _columns(t, name, rows, dtype, tokens=None):
+    """Checks a (rows, tokens) activation matrix; returns its leading dimension."""
+    if t.dtype != dtype or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise TypeError("%s must be a 2-D %s tensor with unit token stride" % (name, dtype))
+    if t.shape[0] != rows or (tokens is not None and t.shape[1] != tokens):
+        raise ValueError("%s must have shape (%d, %s), got %r" % (name, rows, "tokens" if tokens is None else tokens, tuple(t.shape)))
+    n = t.shape[1]
+    if rows > 1 and t.stride(0) < n:
+        raise ValueError("rows of %s overlap (row stride %d < %d tokens)" % (name, t.stride(0), n))
+    return t.stride(0) if rows > 1 else max(n, 1)
+
+
+def _indices(t, name, size):
+    import torch
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous 1-D int32 tensor" % name)
+    if t.shape[0] != size:
+        raise ValueError("%s must have %d entries, got %d" % (name, size, t.shape[0]))
+
+
+def _on(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and (not t.is_cuda or t.device != device):
+            raise ValueError("%s must live on %s (got %s)" % (name, device, t.device))
+
+
+def _natural(**numbers):
+    for name, n in numbers.items():
+        if isinstance(n, bool) or int(n) != n or not 0 <= n < 2 ** 31:
+            raise ValueError("%s must be a whole number from 0 to 2^31 - 1, got %r" % (name, n))
+
+
+class KVCache:
+    """Keys and values of many sequences in 4 bits, in pages on a GPU (the format is shflbw_kv_cache's).
+
+    Activations are (heads * head_dim, tokens) as ``Matrix.spmm`` takes and leaves them.  Slot
+    ``page * page_tokens + place`` holds one token; which pages a sequence has is the caller's bookkeeping.
+    The memory is this object's: one torch uint8 tensor, zeros at first."""
+
+    def __init__(self, pages, page_tokens, heads, head_dim, dtype, device="cuda:0"):
+        import torch
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise TypeError("dtype must be float16 or bfloat16")
+        _natural(pages=pages, page_tokens=page_tokens, heads=heads, head_dim=head_dim)
+        size = int(lib().shflbw_kv_cache_bytes(pages, page_tokens, heads, head_dim))
+        if size == 0 or pages * page_tokens >= 2 ** 31:
+            raise ValueError("a cache has pages of a power of two from 32 to 1024 tokens, fewer than 2^31 slots and "
+                             "head_dim 64, 96 or 128 (got %d pages of %d, %d heads of %d)" % (pages, page_tokens, heads, head_dim))
+        self.pages, self.page_tokens, self.heads, self.head_dim, self.dtype = pages, page_tokens, heads, head_dim, dtype
+        self._dev = torch.zeros(size, dtype=torch.uint8, device=device)
+        self._c = _Cache(self._dev.data_ptr(), pages, page_tokens, heads, head_dim, BF16 if dtype == torch.bfloat16 else F16)
+
+    @property
+    def device(self):
+        return self._dev.device
+
+    def device_bytes(self):
+        return self._dev.numel()
+
+    def write(self, k, v, slots, stream=None):
+        """Quantises column t of k and v into slot ``slots[t]`` (int32, on the GPU); slots outside the cache are skipped."""
+        rows = self.heads * self.head_dim
+        ldk = _columns(k, "k", rows, self.dtype)
+        ldv = _columns(v, "v", rows, self.dtype, k.shape[1])
+        _indices(slots, "slots", k.shape[1])
+        _on(self.device, k=k, v=v, slots=slots)
+        _check(lib().shflbw_kv_write(self._c, k.data_ptr(), ldk, v.data_ptr(), ldv, slots.data_ptr(), k.shape[1],
+                                     _stream_ptr(stream)))
+
+    def read(self, slots, k=None, v=None, stream=None):
+        """(k, v) of the slots, (heads * head_dim, len(slots)) each; NaN for slots outside the cache."""
+        import torch
+        n, rows = slots.shape[0] if slots.dim() else 0, self.heads * self.head_dim
+        _indices(slots, "slots", n)
+        _on(self.device, slots=slots, k=k, v=v)
+        k, v = (torch.empty((rows, n), dtype=self.dtype, device=self.device) if t is None else t for t in (k, v))
+        ldk, ldv = _columns(k, "k", rows, self.dtype, n), _columns(v, "v", rows, self.dtype, n)
+        _check(lib().shflbw_kv_read(self._c, slots.data_ptr(), n, k.data_ptr(), ldk, v.data_ptr(), ldv, _stream_ptr(stream)))
+        return k, v
+
+    def attention(self, q, table, lengths, starts=None, max_queries=1, max_length=None, window=0, sinks=0, out=None, stream=None):
+        """Attention of the last tokens of every sequence over the cache, their own keys and values in it already.
+
+        q (q_heads * head_dim, tokens): sequence b's queries are columns ``starts[b]`` to ``starts[b + 1] - 1``; without
+        starts every sequence has one, column b.  table (batch, pages) int32: the sequence's pages in order.
+        lengths (batch,) int32: its tokens in the cache.  max_queries and max_length: at least what any sequence has
+        (max_length: all of the table's pages by default).  window 0 is none; the first ``sinks`` tokens stay visible
+        past it.  What is on the GPU is not looked at by the host: see shflbw_kv_sequences for what bad entries do."""
+        import torch
+        if q.dtype != self.dtype or q.dim() != 2 or q.shape[0] == 0 or q.shape[0] % (self.heads * self.head_dim):
+            raise TypeError("q must be a 2-D %s tensor with a multiple of %d rows" % (self.dtype, self.heads * self.head_dim))
+        rows, tokens = q.shape
+        ldq = _columns(q, "q", rows, self.dtype)
+        if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1) or table.shape[1] < 1:
+            raise TypeError("table must be a 2-D int32 tensor with unit page stride and a page or more")
+        batch, width = table.shape
+        if batch > 1 and table.stride(0) < width:
+            raise ValueError("rows of table overlap")
+        _indices(lengths, "lengths", batch)
+        if starts is not None:
+            _indices(starts, "starts", batch + 1)
+        elif tokens != batch or max_queries != 1:
+            raise ValueError("without starts every sequence has one query: q must have %d columns, max_queries be 1" % batch)
+        max_length = width * self.page_tokens if max_length is None else max_length
+        _natural(max_queries=max_queries, max_length=max_length, window=window, sinks=sinks)
+        _on(self.device, q=q, table=table, lengths=lengths, starts=starts, out=out)
+        if out is None:
+            out = torch.empty((rows, tokens), dtype=self.dtype, device=self.device)
+        ldo = _columns(out, "out", rows, self.dtype, tokens)
+        s = _Sequences(rows // self.head_dim, batch, max_queries, width, window, sinks, tokens, max_length,
+                       table.stride(0) if batch > 1 else width, table.data_ptr(), lengths.data_ptr(),
+                       None if starts is None else starts.data_ptr())
+        size = _check(lib().shflbw_kv_attention_workspace(self._c, s))
+        work = None
+        if size:
+            # memory of the stream that the work runs on: what was there before it, and what comes after, is ordered with it
+            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+                work = torch.empty(size, dtype=torch.uint8, device=self.device)
+        _check(lib().shflbw_kv_attention(self._c, s, q.data_ptr(), ldq, out.data_ptr(), ldo, work.data_ptr() if size else None, size,
+                                         _stream_ptr(stream)))
+        return out
+
+
+def window_attention(q, k, v, head_dim, starts=None, max_tokens=None, window=0, sinks=0, out=None, stream=None):
+    """Causal attention of prompts to themselves: q (q_heads * head_dim, tokens), k and v (heads * head_dim, tokens).
+
+    Sequence b is columns ``starts[b]`` to ``starts[b + 1] - 1`` (int32, on the GPU); without starts all columns are one.
+    max_tokens: at least the longest sequence's tokens (all of them by default).  A key at j is visible from p if
+    j <= p and (window 0, or p - j < window, or j < sinks)."""
+    import torch
+    if q.dtype not in (torch.float16, torch.bfloat16) or q.dim() != 2 or k.dim() != 2:
+        raise TypeError("q, k and v must be 2-D float16 or bfloat16 tensors")
+    _natural(head_dim=head_dim, window=window, sinks=sinks)
+    rows, tokens = q.shape
+    if head_dim == 0 or rows == 0 or k.shape[0] == 0 or k.shape[0] % head_dim or rows % k.shape[0]:
+        raise ValueError("q's rows must be a multiple of k's, and those of head_dim = %d (got %d and %d)" % (head_dim, rows, k.shape[0]))
+    ldq = _columns(q, "q", rows, q.dtype)
+    ldk, ldv = _columns(k, "k", k.shape[0], q.dtype, tokens), _columns(v, "v", k.shape[0], q.dtype, tokens)
+    sequences = 1
+    if starts is not None:
+        sequences = starts.shape[0] - 1 if starts.dim() == 1 and starts.shape[0] else 0
+        _indices(starts, "starts", sequences + 1)
+    max_tokens = tokens if max_tokens is None else max_tokens
+    _natural(max_tokens=max_tokens)
+    _on(q.device, q=q, k=k, v=v, starts=starts, out=out)
+    if out is None:
+        out = torch.empty((rows, tokens), dtype=q.dtype, device=q.device)
+    ldo = _columns(out, "out", rows, q.dtype, tokens)
+    _check(lib().shflbw_window_attention(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, out.data_ptr(), ldo,
+                                         rows // head_dim, k.shape[0] // head_dim, head_dim, tokens,
+                                         None if starts is None else starts.data_ptr(), sequences, max_tokens, window, sinks,
+                                         BF16 if q.dtype == torch.bfloat16 else F16, _stream_ptr(stream)))
     return out
 
 
