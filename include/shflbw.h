@@ -358,7 +358,7 @@ int shflbw_kv_attention(const shflbw_kv_cache* cache, const shflbw_kv_sequences*
  *  window  the key at j is visible from p if j <= p and (window 0, or p - j <
  *          window, or j < sinks)
  * Accuracy, hidden keys and values, and determinism as in shflbw_kv_attention.
- * Any alignment and leading dimension.  Enqueues on `stream` only.
+ * Any alignment; ldk and ldv below 2^26.  Enqueues on `stream` only.
  */
 int shflbw_window_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
                             void* out, int64_t ldo, int q_heads, int heads, int head_dim, int64_t tokens,

@@ -59,14 +59,15 @@ struct AttnArgs {
     int col_blocks;           // blocks of columns of a sequence and key head
 };
 
-constexpr int ATTN_WAVES = 8;            // wavefronts of a workgroup
 constexpr int ATTN_DECODE_KEYS = 32;     // keys of a tile of the decoding kernel
 constexpr int ATTN_TILE_KEYS = 64;       // keys of a tile of the other
-constexpr int ATTN_TILE_QUERIES = 32;    // queries of a wavefront there
+constexpr int ATTN_TILE_QUERIES = 32;    // queries of an item there
+constexpr int64_t ATTN_MAX_LD = 1 << 26;  // of a prompt's keys and values: 32 rows span less than 4 GiB
 
 struct AttnPlan {
     bool decode;              // the kernel for few queries
     int col_tiles;            // its 16-column tiles per wavefront
+    int waves;                // the other's wavefronts per workgroup
     int col_blocks, splits, split_tiles;
     int64_t groups;           // workgroups
     int64_t workspace;        // bytes

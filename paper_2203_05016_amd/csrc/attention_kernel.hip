@@ -18,6 +18,7 @@
 
 #include <cfloat>
 #include <cstdint>
+#include <type_traits>
 
 #include "attention.h"
 
@@ -436,10 +437,23 @@ __global__ __launch_bounds__(64 * W) void attention_decode_kernel(AttnArgs a)
 
 // ---- tiles of queries
 //
-// A workgroup takes one sequence and key head and 8 items, one per wavefront: 32 neighbouring queries of one of the
-// group's heads; heads vary fastest, so that grouped heads share the tiles of keys and values.  Tiles of 64 keys are brought to the LDS
-// by all wavefronts, the next while this one is worked on: from the cache unpacked, [key][feature]; from a prompt as they lie,
-// [feature][key].  What lies the wrong way for its product is turned by transposing reads.
+// A workgroup of W wavefronts takes one sequence and key head and W items, one per wavefront: 32 neighbouring queries of one of
+// the group's heads; heads vary fastest, so that grouped heads share the tiles of keys and values.
+//
+// Tiles of 64 keys are brought to one of three LDS buffers by all wavefronts, two tiles ahead in registers, one in the
+// LDS: from the cache unpacked, [key][feature]; from a prompt as they lie, [feature][key].  What lies the wrong way for its product is
+// turned by transposing reads.  One barrier per tile.
+//
+// A wavefront works on 32 keys at a time, three of them at once: the scores of the next, the softmax of this one, the second product
+// of the one before.  Matrix and vector instructions of such a step do not depend on each other, so that one wavefront issues
+// the latter while the former run.  The maximum that scores are taken off follows the true one only when that has grown by
+// ATTN_SLACK powers of two: rescaling the accumulators is rare then, and weights stay below 2^ATTN_SLACK.
+//
+// Infinities and NaN among the values of a tile that not all of the workgroup's queries see whole are zeros in the LDS, so that
+// they do not reach a query that does not see them as 0 * NaN; if there were any, they are added where they are seen at the end.
+constexpr float ATTN_SLACK = 8;
+constexpr int ATTN_AHEAD = 2;              // an operand is read this many steps of the reduction before its product
+
 template <bool BF, int D, bool CACHE>
 struct AttnStage {
     // LDS pitches in bytes.  Cache: an odd number of 16-byte units for the keys (16 lanes read 16 rows), 64 bytes past a
@@ -453,19 +467,28 @@ struct AttnStage {
 // 16-byte unit u of a row of 64 tokens lies at unit u ^ attn_unit(row): the rows of 16 lanes' reads, and the 64-byte
 // pieces of four neighbouring rows, fall into different banks
 __device__ __forceinline__ int attn_unit(int row) { return ((row >> 1 & 1) << 2) | (row >> 2 & 1) << 1 | (row >> 3 & 1); }
+// the largest of three, without the rewriting of signalling NaN that fmaxf comes with
+__device__ __forceinline__ float attn_max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 
-template <bool BF, int D, bool CACHE>
-__global__ __launch_bounds__(64 * ATTN_WAVES, 2) void attention_tile_kernel(AttnArgs a)
+template <bool BF, int D, bool CACHE, int W>
+__global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
 {
     using Stage = AttnStage<BF, D, CACHE>;
     constexpr int S = D / 16, DT = D / 32, KP = Stage::KP, VP = Stage::VP;
     constexpr int SB = scale_bytes(D);
-    constexpr int UNITS = D / 32;                          // 16-byte units of a tile per thread (prompt), words (cache)
-    __shared__ __attribute__((aligned(16))) char smem[2][Stage::BYTES];
-    __shared__ int special[2];                             // tile of the buffer that holds an infinity or a NaN among its values
+    constexpr int KINDS = W == 8 ? 1 : 2;                  // four wavefronts bring keys and values, of eight each four one of them
+    constexpr int UNITS = D / 32;                          // 16-byte units of a tile (cache: words) per thread and kind
+    constexpr int PARTS = KINDS * UNITS;
+    __shared__ __attribute__((aligned(16))) char smem[3 * Stage::BYTES];
+    __shared__ int special;                                // whether values were replaced by zeros
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int half = lane >> 5, c = lane & 31;
+    const int half = lane >> 5, c = lane & 31, r = lane & 15;
     // a sequence and key head's workgroups on one XCD, whose L2 holds its keys and values; those with most keys first
     const int per_pair = a.col_blocks * a.splits;
     const int pair = (int)(blockIdx.x % 8 + blockIdx.x / 8 / per_pair * 8), inner = blockIdx.x / 8 % per_pair;
@@ -475,9 +498,9 @@ __global__ __launch_bounds__(64 * ATTN_WAVES, 2) void attention_tile_kernel(Attn
 
     const AttnSeq seq = attn_sequence<CACHE>(a, b);
     const int blocks = (seq.nq + ATTN_TILE_QUERIES - 1) / ATTN_TILE_QUERIES;
-    const int64_t items = (int64_t)blocks * a.group, item0 = (int64_t)blk * ATTN_WAVES;
+    const int64_t items = (int64_t)blocks * a.group, item0 = (int64_t)blk * W;
     if (item0 >= items) return;
-    const int64_t item_last = items < item0 + ATTN_WAVES ? items - 1 : item0 + ATTN_WAVES - 1;
+    const int64_t item_last = items < item0 + W ? items - 1 : item0 + W - 1;
     const int shift = CACHE ? 0 : (int)(seq.t0 & 7);       // tiles of a prompt begin at multiples of 8 columns
     const int p0 = seq.len - seq.nq;
     const auto position = [&](int64_t query) { return p0 + (int)(query < seq.nq ? query : seq.nq - 1); };
@@ -487,18 +510,18 @@ __global__ __launch_bounds__(64 * ATTN_WAVES, 2) void attention_tile_kernel(Attn
     const int v_begin = split * (a.splits > 1 ? a.split_tiles : 0);
     const int v_end = a.splits == 1 || tiles.count - v_begin < a.split_tiles ? tiles.count : v_begin + a.split_tiles;
 
+    // the wavefront's item; one that is not there repeats the last one, needs no keys, and its result is dropped
     const bool works = item0 + wave <= item_last;
     const int64_t item = works ? item0 + wave : item_last;
-    const int head = h * a.group + (int)(item % a.group);
-    const int query = (int)(item / a.group) * ATTN_TILE_QUERIES + c;
-    const int first = position(query - c), last = position(query - c + ATTN_TILE_QUERIES - 1), p = position(query);
-    const int lo = attn_window_start(p, a.window);
-    const int64_t token = seq.t0 + (query < seq.nq ? query : seq.nq - 1);
+    const int head = h * a.group + (int)(item % a.group), q0 = (int)(item / a.group) * ATTN_TILE_QUERIES, query = q0 + c;
+    const int p = position(query), lo = attn_window_start(p, a.window);
+    const int first = works ? position(q0) : INT32_MAX, last = works ? position(q0 + ATTN_TILE_QUERIES - 1) : -1;
+    const int window_first = attn_window_start(first, a.window), window_last = attn_window_start(last, a.window);
 
     // queries: lane c has column c; features 16 s + 8 half and up
     uint4v q[S];
     {
-        const uint16_t* src = a.q + ((int64_t)head * D + 8 * half) * a.ldq + token;
+        const uint16_t* src = a.q + ((int64_t)head * D + 8 * half) * a.ldq + seq.t0 + (query < seq.nq ? query : seq.nq - 1);
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
@@ -506,196 +529,356 @@ __global__ __launch_bounds__(64 * ATTN_WAVES, 2) void attention_tile_kernel(Attn
                 q[s][i] = src[(int64_t)(16 * s + 2 * i) * a.ldq] | (unsigned)src[(int64_t)(16 * s + 2 * i + 1) * a.ldq] << 16;
     }
 
-    // ---- staging
+    // the first key of tile v
+    const int key_sinks = -shift, key_window = (tiles.window - tiles.sinks) * ATTN_TILE_KEYS - shift;
+    const auto first_key = [&](int v) __attribute__((always_inline)) { return v * ATTN_TILE_KEYS + (v < tiles.sinks ? key_sinks : key_window); };
+    // whether not all of the workgroup's queries see all 64 keys from j on
+    const int wg_window = attn_window_start(wg_last, a.window);
+    const auto partial = [&](int j) __attribute__((always_inline)) {
+        return j < 0 || j + ATTN_TILE_KEYS - 1 > wg_first || (j < wg_window && j + ATTN_TILE_KEYS - 1 >= a.sinks);
+    };
+    // of 32 keys from j on: whether any of the wavefront's queries sees any, or not all see all
+    const auto is_needed = [&](int j) __attribute__((always_inline)) { return j <= last && j + 31 >= 0 && (j + 31 >= window_first || j < a.sinks); };
+    const auto is_masked = [&](int j) __attribute__((always_inline)) { return j < 0 || j + 31 > first || (j < window_last && j + 31 >= a.sinks); };
+
+    // ---- staging: memory -> registers -> LDS, a part at a time, to be spread among the products
     const int page = 1 << a.page_shift;
-    const int64_t chunk = page_head_bytes(page, D);
+    const int64_t chunk = page_head_bytes(page, D), page_bytes = chunk * a.heads;
+    const char* pages = CACHE ? a.cache + h * chunk : nullptr;
     const int32_t* table = CACHE ? a.table + (int64_t)b * a.table_ld : nullptr;
-    const int kind = tid >> 8, sub = tid >> 6 & 3;         // cache: keys or values, 16 of a tile's keys
-    const int row = kind ? ((lane >> 4) & 1) * 8 + ((lane >> 1) & 7) : lane & 15;      // the thread's key among these
-    const int part = kind ? (lane & 1) + 2 * (lane >> 5) : lane >> 4;                  // and its words' 8 features of 32
-    uint4v unit[CACHE ? 1 : UNITS];
-    unsigned word[CACHE ? UNITS : 1], codes = 0;
-    const auto load = [&](int v) __attribute__((always_inline)) {
-        const int t = tiles.real(v);
+    const int kind0 = W == 8 ? wave >> 2 : 0, brings = wave & 3, member = tid & 255;
+    uint4v unit[KINDS][CACHE ? 1 : UNITS];
+    unsigned word[KINDS][CACHE ? UNITS : 1], codes[KINDS] = {};
+    int page_id = -1;                                      // cache: of the wavefront's keys of the next tile to load
+    bool known = false, known_before = false;              // whether there is such a page: of the tile just loaded, of the one before
+    const char* from[KINDS];                               // of the next tile to load, the same for all lanes of a wavefront
+    const char* scales_from[KINDS];
+    int64_t row_step[KINDS];                               // prompt: bytes of 32 rows
+    int64_t left[KINDS];                                   // and from there to the last 16 bytes of the tensor, or much
+    unsigned lane_off[KINDS], scale_off[KINDS];            // a lane's bytes past these
+    int lds_off[KINDS];
+#pragma unroll
+    for (int n = 0; n < KINDS; ++n) {
+        const int kind = kind0 + n;
         if constexpr (CACHE) {
-            const int key = t * ATTN_TILE_KEYS + sub * 16;
-            const int idx = key >> a.page_shift, at = key & (page - 1);
-            const int id = idx < a.table_width ? table[idx] : -1;
-            const bool known = (unsigned)id < (unsigned)a.pages;
-            const char* base = a.cache + ((int64_t)(known ? id : 0) * a.heads + h) * chunk;
-            const unsigned* src = reinterpret_cast<const unsigned*>(base + (int64_t)kind * page * D / 2 + code_offset(D, at, lane));
-#pragma unroll
-            for (int s = 0; s < UNITS; ++s) word[s] = src[s];
-            const char* sc = base + (int64_t)page * D + (int64_t)(kind * page + at + row) * SB;
-            codes = SB == 2 ? *reinterpret_cast<const uint16_t*>(sc) : *reinterpret_cast<const unsigned*>(sc);
-            if (!known) codes = 0xffffffffu;               // a page that is not there reads as NaN
+            const int row = kind ? ((lane >> 4) & 1) * 8 + ((lane >> 1) & 7) : r, part = kind ? (lane & 1) + 2 * half : lane >> 4;
+            lane_off[n] = (D == 64 ? lane * 16 : lane * (D / 8)) + kind * page * (D / 2);
+            scale_off[n] = page * D + (kind * page + row) * SB;
+            lds_off[n] = kind ? Stage::K_BYTES + (brings * 16 + row) * VP + part * 16 : (brings * 16 + row) * KP + part * 16;
         } else {
-#pragma unroll
-            for (int i = 0; i < UNITS; ++i) {
-                const int e = tid + 512 * i, f = (e >> 3) % D;
-                const bool is_v = e >= 8 * D;
-                const int64_t at = seq.t0 - shift + (int64_t)t * ATTN_TILE_KEYS + (e & 7) * 8;
-                const uint16_t* src = (is_v ? a.v : a.k) + ((int64_t)h * D + f) * (is_v ? a.ldv : a.ldk);
-                uint4v x = {0, 0, 0, 0};
-                if (at + 8 <= a.tokens) {
-                    __builtin_memcpy(&x, src + at, 16);
-                } else {
-                    for (int j = 0; j < 8; ++j)
-                        if (at + j < a.tokens) x[j >> 1] |= (unsigned)src[at + j] << 16 * (j & 1);
-                }
-                unit[i] = x;
-            }
+            const int64_t ld = kind ? a.ldv : a.ldk;
+            const int f = member >> 3;                     // rows f + 32 i have the same attn_unit
+            row_step[n] = 64 * ld;
+            lane_off[n] = 2 * ((unsigned)f * (unsigned)ld + (member & 7) * 8);
+            lds_off[n] = (kind ? Stage::K_BYTES : 0) + f * 128 + ((member & 7) ^ attn_unit(f)) * 16;
+            left[n] = INT64_MAX;
+        }
+    }
+    const auto find_page = [&](int j) __attribute__((always_inline)) {
+        if constexpr (CACHE) {
+            const int idx = (j + brings * 16) >> a.page_shift;
+            page_id = table[idx < a.table_width ? idx : a.table_width - 1];   // (keys past the last page are hidden)
         }
     };
-    const auto store = [&](int v) __attribute__((always_inline)) {
-        char* buf = smem[v & 1];
+    // What lies past a row's last column (the next row, or what is between them) is brought as well and hidden.  Past the last row's
+    // nothing is read: there the last 8 values are read, and moved to their places before they go to the LDS.
+    const auto at_end = [&](int j) __attribute__((always_inline)) { return !CACHE && h == a.heads - 1 && seq.t0 + j + ATTN_TILE_KEYS > a.tokens; };
+    // the tile whose keys are j and up; next: those of the tile after it
+    const auto load_begin = [&](int j, int next) __attribute__((always_inline)) {
+        if constexpr (CACHE) {
+            const int at = (j + brings * 16) & (page - 1);     // a wavefront brings 16 keys (and their values)
+            known = (unsigned)page_id < (unsigned)a.pages;
+            const char* base = pages + (known ? page_id : 0) * page_bytes;
+#pragma unroll
+            for (int n = 0; n < KINDS; ++n) {
+                from[n] = base + code_offset(D, at, 0);
+                scales_from[n] = base + at * SB;
+            }
+            find_page(next);
+        } else {
+            const int64_t tile = seq.t0 + j;
+#pragma unroll
+            for (int n = 0; n < KINDS; ++n) from[n] = reinterpret_cast<const char*>((kind0 + n ? a.v : a.k) + (int64_t)h * D * (kind0 + n ? a.ldv : a.ldk) + tile);
+            if (at_end(j))
+#pragma unroll
+                for (int n = 0; n < KINDS; ++n) left[n] = 2 * (((int64_t)D - 1) * (kind0 + n ? a.ldv : a.ldk) + a.tokens - 8 - tile);
+        }
+    };
+    const auto most = [&](int n, int u) __attribute__((always_inline)) {   // the last offset from unit u's rows on
+        const int64_t x = left[n] - u * row_step[n];
+        return x < 0xffffffffLL ? (unsigned)x : 0xffffffffu;
+    };
+    const auto load_part = [&](int i) __attribute__((always_inline)) {
+        if constexpr (CACHE) {
+            if (i >= KINDS) return;
+            const unsigned* src = reinterpret_cast<const unsigned*>(from[i] + lane_off[i]);
+#pragma unroll
+            for (int s = 0; s < UNITS; ++s) word[i][s] = src[s];
+            const char* sc = scales_from[i] + scale_off[i];
+            codes[i] = SB == 2 ? *reinterpret_cast<const uint16_t*>(sc) : *reinterpret_cast<const unsigned*>(sc);
+        } else {
+            const int n = i / UNITS, u = i % UNITS;
+            const unsigned end = most(n, u), off = lane_off[n] < end ? lane_off[n] : end;
+            __builtin_memcpy(&unit[n][u], from[n] + u * row_step[n] + off, 16);
+        }
+    };
+    const auto store_begin = [&](int j, bool clean) __attribute__((always_inline)) {
+        if constexpr (CACHE) {
+            if (!known_before)                             // a page that is not there reads as NaN
+#pragma unroll
+                for (int n = 0; n < KINDS; ++n) codes[n] = 0xffffffffu;
+        } else if (at_end(j)) {
+#pragma unroll
+            for (int n = 0; n < KINDS; ++n)
+#pragma unroll
+                for (int i = 0; i < UNITS; ++i) {
+                    const unsigned end = most(n, i), by = lane_off[n] > end ? (lane_off[n] - end) / 2 : 0;
+                    uint64_t x = unit[n][i][0] | (uint64_t)unit[n][i][1] << 32, y = unit[n][i][2] | (uint64_t)unit[n][i][3] << 32;
+                    const int bits = (int)(by & 3) * 16;
+                    if (by >= 4) { x = y; y = 0; }
+                    if (bits) { x = x >> bits | y << (64 - bits); y >>= bits; }
+                    if (by >= 8) x = y = 0;
+                    unit[n][i] = uint4v{(unsigned)x, (unsigned)(x >> 32), (unsigned)y, (unsigned)(y >> 32)};
+                }
+        }
+        if (!clean || kind0 + KINDS == 1) return;
+        constexpr int n = KINDS - 1;
         bool found = false;
         if constexpr (CACHE) {
-            char* dst = buf + (kind ? Stage::K_BYTES + (sub * 16 + row) * VP : (sub * 16 + row) * KP) + part * 16;
 #pragma unroll
-            for (int s = 0; s < UNITS; ++s) {
-                found |= kind && (codes >> 8 * s & 255) == 255;
-                *reinterpret_cast<uint4v*>(dst + s * 64) = attn_unpack<BF>(word[s], codes >> 8 * s & 255);
-            }
+            for (int s = 0; s < UNITS; ++s)
+                if ((codes[n] >> 8 * s & 255) == 255) {
+                    found = true;
+                    codes[n] &= ~(255u << 8 * s);
+                    word[n][s] = 0;
+                }
         } else {
             constexpr unsigned EXP = BF ? 0x7f80u : 0x7c00u;
 #pragma unroll
-            for (int i = 0; i < UNITS; ++i) {
-                const int e = tid + 512 * i, f = (e >> 3) % D;
-                const bool is_v = e >= 8 * D;
-                *reinterpret_cast<uint4v*>(buf + (is_v ? Stage::K_BYTES : 0) + f * 128 + ((e & 7) ^ attn_unit(f)) * 16) = unit[i];
+            for (int i = 0; i < UNITS; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    found |= is_v && ((unit[i][j] & EXP) == EXP || (unit[i][j] >> 16 & EXP) == EXP);
-            }
+                for (int k = 0; k < 4; ++k) {
+                    const unsigned x = unit[n][i][k];
+                    const bool lo_bad = (x & EXP) == EXP, hi_bad = (x >> 16 & EXP) == EXP;
+                    found |= lo_bad | hi_bad;
+                    unit[n][i][k] = x & (lo_bad ? 0xffff0000u : ~0u) & (hi_bad ? 0xffffu : ~0u);
+                }
         }
-        if (found) special[v & 1] = v;
+        if (found) special = 1;
+    };
+    const auto store_part = [&](int i, int buffer) __attribute__((always_inline)) {
+        const int n = i / UNITS, u = i % UNITS;
+        char* dst = smem + buffer + lds_off[n];
+        if constexpr (CACHE) *reinterpret_cast<uint4v*>(dst + u * 64) = attn_unpack<BF>(word[n][u], codes[n] >> 8 * u & 255);
+        else *reinterpret_cast<uint4v*>(dst + u * 4096) = unit[n][u];
     };
 
-    float16v o[DT] = {};
+    // ---- products
+    const attn_lds lds = (attn_lds)smem;
+    int k_at[2], v_at[4];
+    if constexpr (CACHE) {
+        k_at[0] = c * KP + half * 16;
+        v_at[0] = Stage::K_BYTES + (4 * half + (r >> 2)) * VP + (16 * (lane >> 4 & 1) + (r & 3) * 4) * 2;
+    } else {
+        // rows 8 x + 4 half + i of the scores' tile are to be keys 16 .. + 8 half + 4 x + i: the two middle groups of
+        // four of every 16 change places
+        const int f = 8 * half + (r >> 2), at = 16 * (lane >> 4 & 1) + ((r & 1) << 1 | (r >> 1 & 1)) * 4;   // the first of four keys
+        k_at[0] = f * 128 + ((at >> 3) ^ attn_unit(f)) * 16 + (at & 4) * 2;
+        k_at[1] = (f + 4) * 128 + ((at >> 3) ^ attn_unit(f + 4)) * 16 + (at & 4) * 2;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) v_at[g] = Stage::K_BYTES + c * 128 + ((2 * g + half) ^ attn_unit(c)) * 16;
+    }
+    // the first operand of the scores of keys 32 sub and up, at step s; buf: the tile's buffer, in bytes
+    const auto key_operand = [&](int buf, int sub, int s) __attribute__((always_inline)) {
+        if constexpr (CACHE) {
+            return *(const __attribute__((address_space(3))) uint4v*)(lds + buf + k_at[0] + sub * 32 * KP + s * 32);
+        } else {
+            const uint2 one = attn_transposed(lds + buf + (k_at[0] ^ sub * 64) + s * 2048);
+            const uint2 two = attn_transposed(lds + buf + (k_at[1] ^ sub * 64) + s * 2048);
+            return uint4v{one.x, one.y, two.x, two.y};
+        }
+    };
+    // that of the second product: features 32 t and up, keys 16 g and up
+    const auto value_operand = [&](int buf, int g, int t) __attribute__((always_inline)) {
+        if constexpr (CACHE) {
+            const uint2 one = attn_transposed(lds + buf + v_at[0] + g * 16 * VP + t * 64), two = attn_transposed(lds + buf + v_at[0] + (g * 16 + 8) * VP + t * 64);
+            return uint4v{one.x, one.y, two.x, two.y};
+        } else {
+            return *(const __attribute__((address_space(3))) uint4v*)(lds + buf + v_at[g] + t * 4096);
+        }
+    };
+
+    float16v o[DT] = {}, sc[2] = {};                       // two sets of scores, each of 32 keys ..
+    uint4v w[2][2] = {};                                   // .. and of weights
     float m = -FLT_MAX, l = 0;
 
-    if (tid < 2) special[tid] = -1;
-    if (v_begin < v_end) load(v_begin);
-    __syncthreads();
-    if (v_begin < v_end) store(v_begin);
-
-    for (int v = v_begin; v < v_end; ++v) {
-        __syncthreads();
-        if (v + 1 < v_end) load(v + 1);
-        const int j0 = tiles.real(v) * ATTN_TILE_KEYS - shift, j1 = j0 + ATTN_TILE_KEYS - 1;
-        const bool needed = works && j0 <= last && j1 >= 0 && (j1 >= attn_window_start(first, a.window) || j0 < a.sinks);
-        if (needed) {
-            const char* kb = smem[v & 1];
-            const char* vb = kb + Stage::K_BYTES;
-            const bool masked = j0 < 0 || j1 > first || (j0 < attn_window_start(last, a.window) && j1 >= a.sinks);
-            float16v sc[2] = {};
+    // half SUB of a tile, keys j and up, whose scores are in sc[SUB]: its weights; beside it the other half's scores (of the
+    // next tile, where SUB is 1), the product of the weights before, and a part of the staging.  part: the tile is a partial one.
+    const auto step = [&](auto which, int j, bool part, int next_buf, int last_buf, int stage_buf, int j_before, int j_after) __attribute__((always_inline)) {
+        constexpr int SUB = decltype(which)::value;
+        const auto stage = [&](int i) __attribute__((always_inline)) {
+            if constexpr (SUB == 0) store_part(i, stage_buf);
+            else load_part(i);
+        };
+        if (part) {
+            // nothing to compute where neither these keys nor their neighbours in order are needed
+            if (!(is_needed(j) || is_needed(j_before) || is_needed(j_after))) {
 #pragma unroll
-            for (int s = 0; s < S; ++s)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    uint4v x;
-                    if constexpr (CACHE) {
-                        x = *reinterpret_cast<const uint4v*>(kb + (32 * t + c) * KP + (2 * s + half) * 16);
-                    } else {
-                        // rows 8 x + 4 half + i of the scores' tile are to be keys 16 .. + 8 half + 4 x + i: the two
-                        // middle groups of four of every 16 change places
-                        const int i = lane & 15, f = 16 * s + 8 * half + (i >> 2);
-                        const int at = 32 * t + 16 * (lane >> 4 & 1) + ((i & 1) << 1 | (i >> 1 & 1)) * 4;   // first of four keys
-                        const uint2 one = attn_transposed((attn_lds)kb + f * 128 + ((at >> 3) ^ attn_unit(f)) * 16 + (at & 4) * 2);
-                        const uint2 two = attn_transposed((attn_lds)kb + (f + 4) * 128 + ((at >> 3) ^ attn_unit(f + 4)) * 16 + (at & 4) * 2);
-                        x = uint4v{one.x, one.y, two.x, two.y};
-                    }
-                    sc[t] = attn_mma32<BF>(x, q[s], sc[t]);
-                }
-            // key of the scores' register i of tile t
-            const auto key = [&](int t, int i) __attribute__((always_inline)) {
-                return j0 + 32 * t + (CACHE ? 8 * (i >> 2) + 4 * half + (i & 3) : 16 * (i >> 3) + 8 * half + (i & 7));
-            };
-            float top = -INFINITY;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
+                for (int i = 0; i < PARTS; ++i) stage(i);
+                w[SUB][0] = w[SUB][1] = uint4v{};
+                return;
+            }
+            if (is_masked(j))
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    if (masked && !attn_sees(key(t, i), p, lo, a.sinks)) sc[t][i] = -INFINITY;
-                    top = fmaxf(top, sc[t][i]);
+                    const int k = j + (CACHE ? 8 * (i >> 2) + 4 * half + (i & 3) : 16 * (i >> 3) + 8 * half + (i & 7));
+                    if (!attn_sees(k, p, lo, a.sinks)) sc[SUB][i] = -INFINITY;
                 }
-            const float2v both = attn_pair32(top);
-            top = fmaxf(both[0], both[1]) * a.scale;
-            if (__any(top > m)) {
-                const float now = fmaxf(m, top), shrink = attn_exp2(m - now);
+        }
+        // Pieces of all that, in an order that keeps both units busy: per step of the reduction an operand of each product is
+        // read ATTN_AHEAD steps before its use, two products are issued, and a share of the vector work follows: the maximum, whether
+        // to follow it, and the weights two at a time
+        float16v& x = sc[SUB];
+        float top = 0, shrink = 1;
+        bool grown = false;
+        const auto piece = [&](int u) __attribute__((always_inline)) {
+            if (u == 0) {
+                top = attn_max3(x[0], x[1], x[2]);
+#pragma unroll
+                for (int i = 3; i < 15; i += 2) top = attn_max3(top, x[i], x[i + 1]);
+                top = attn_max3(top, x[15], x[15]);
+            } else if (u == 1) {
+                const float2v both = attn_pair32(top);
+                top = attn_max3(both[0], both[1], both[1]) * a.scale;
+                grown = top > m + ATTN_SLACK;
+                const float now = grown ? top : m;
+                shrink = attn_exp2(m - now);
                 m = now;
                 l *= shrink;
-#pragma unroll
-                for (int t = 0; t < DT; ++t) o[t] *= shrink;
+            } else {
+                const int i = 2 * (u - 2);
+                const float y = attn_exp2(__builtin_fmaf(x[i], a.scale, -m)), z = attn_exp2(__builtin_fmaf(x[i + 1], a.scale, -m));
+                l += y + z;
+                w[SUB][i >> 3][(i & 7) >> 1] = attn_pack<BF>(y, z);
             }
-            uint4v w[4];
+        };
+        uint4v ks[S], xs[S];
+        const auto fetch = [&](int s) __attribute__((always_inline)) {
+            ks[s] = key_operand(next_buf, 1 - SUB, s);
+            xs[s] = value_operand(last_buf, 2 * (1 - SUB) + s / DT, s % DT);
+        };
+        sc[1 - SUB] = float16v{};
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+        for (int s = 0; s < ATTN_AHEAD; ++s) fetch(s);
 #pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float x = attn_exp2(__builtin_fmaf(sc[t][i], a.scale, -m)), y = attn_exp2(__builtin_fmaf(sc[t][i + 1], a.scale, -m));
-                    l += x + y;
-                    w[2 * t + (i >> 3)][(i & 7) >> 1] = attn_pack<BF>(x, y);
-                }
-            // a value at keys that only some of the queries see must not reach the others as 0 * NaN: infinities and
-            // NaN are added where they are seen, and are zeros in the product
-            const bool apart = masked && __builtin_amdgcn_readfirstlane(special[v & 1]) == v;
-            if (apart) {
-                for (int n = 0; n < ATTN_TILE_KEYS; ++n) {
-                    const bool seen = attn_sees(j0 + n, p, lo, a.sinks);
+        for (int s = 0; s < S; ++s) {
+            if (s + ATTN_AHEAD < S) fetch(s + ATTN_AHEAD);
+            sc[1 - SUB] = attn_mma32<BF>(ks[s], q[s], sc[1 - SUB]);
+            o[s % DT] = attn_mma32<BF>(xs[s], w[1 - SUB][s / DT], o[s % DT]);
+#pragma unroll
+            for (int i = s * PARTS / S; i < (s + 1) * PARTS / S; ++i) stage(i);
+#pragma unroll
+            for (int u = s * 10 / S; u < (s + 1) * 10 / S; ++u) piece(u);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // the weights are worked out before the branch, among the products
+        asm volatile("" : "+v"(w[SUB][0]), "+v"(w[SUB][1]), "+v"(l));
+        if (__any(grown))
+#pragma unroll
+            for (int t = 0; t < DT; ++t) o[t] *= shrink;
+    };
+
+    // the first step's product is one of zeros, with the third buffer's values
+    for (int e = tid * 16; e < Stage::V_BYTES; e += 64 * W * 16)
+        *reinterpret_cast<uint4v*>(smem + 2 * Stage::BYTES + Stage::K_BYTES + e) = uint4v{};
+    if (tid == 0) special = 0;
+    // past the last tile that one is brought again, to a buffer that is not read any more
+    const auto clamped = [&](int v) __attribute__((always_inline)) { return first_key(v < v_end ? v : v_end - 1); };
+    int j = clamped(v_begin), j_next = clamped(v_begin + 1);
+    if (v_begin < v_end) {
+        find_page(j);
+        load_begin(j, j_next);
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) load_part(i);
+        known_before = known;
+    }
+    __syncthreads();
+    if (v_begin < v_end) {
+        store_begin(j, partial(j));
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) store_part(i, 0);
+        load_begin(j_next, clamped(v_begin + 2));
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) load_part(i);
+        known_before = known;
+    }
+    __syncthreads();
+    if (v_begin < v_end)
+#pragma unroll
+        for (int s = 0; s < S; ++s) sc[0] = attn_mma32<BF>(key_operand(0, 0, s), q[s], sc[0]);
+    int buf = 0, before = 2 * Stage::BYTES, j_before = INT32_MAX;
+    bool part = partial(j);
+    for (int v = v_begin; v < v_end; ++v) {
+        const int after = buf == 2 * Stage::BYTES ? 0 : buf + Stage::BYTES;
+        const bool part_next = partial(j_next);
+        store_begin(j_next, part_next);
+        step(std::integral_constant<int, 0>{}, j, part, buf, before, after, j_before, j + 32);
+        __syncthreads();
+        const int j_then = clamped(v + 2);
+        load_begin(j_then, clamped(v + 3));
+        step(std::integral_constant<int, 1>{}, j + 32, part, after, buf, 0, j, j_next);
+        known_before = known;
+        j_before = j + 32;
+        j = j_next;
+        j_next = j_then;
+        part = part_next;
+        before = buf;
+        buf = after;
+    }
+    if (v_begin < v_end)
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int t = 0; t < DT; ++t) o[t] = attn_mma32<BF>(value_operand(before, 2 + g, t), w[1][g], o[t]);
+
+    if (special)
+        for (int v = v_begin; v < v_end; ++v) {
+            const int from_key = first_key(v);
+            if (!partial(from_key)) continue;
+            for (int k = from_key; k < from_key + ATTN_TILE_KEYS; ++k) {
+                if (!attn_sees(k, p, lo, a.sinks)) continue;
+                if constexpr (CACHE) {
+                    const int id = table[k >> a.page_shift];
+                    const bool there = (unsigned)id < (unsigned)a.pages;
+                    const char* sc8 = pages + (there ? id : 0) * page_bytes + (int64_t)page * D + (int64_t)(page + (k & (page - 1))) * SB;
+#pragma unroll
+                    for (int t = 0; t < DT; ++t)
+                        if (!there || (unsigned char)sc8[t] == 255) o[t] += __builtin_nanf("");
+                } else {
 #pragma unroll
                     for (int t = 0; t < DT; ++t)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int d = 32 * t + 8 * (i >> 2) + 4 * half + (i & 3);
-                            const uint16_t x = *reinterpret_cast<const uint16_t*>(
-                                CACHE ? vb + n * VP + d * 2 : vb + d * 128 + ((n >> 3) ^ attn_unit(d)) * 16 + (n & 7) * 2);
-                            const float f = attn_widen<BF>(x);
-                            if (seen && !(__builtin_fabsf(f) < INFINITY)) o[t][i] += f;
+                        for (int e = 0; e < 16; ++e) {
+                            const int d = 32 * t + 8 * (e >> 2) + 4 * half + (e & 3);
+                            const float f = attn_widen<BF>(a.v[((int64_t)h * D + d) * a.ldv + seq.t0 + k]);
+                            if (!(__builtin_fabsf(f) < INFINITY)) o[t][e] += f;
                         }
                 }
             }
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-#pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    uint4v x;
-                    if constexpr (CACHE) {
-                        const int i = lane & 15;
-                        const attn_lds at = (attn_lds)vb + (16 * g + 4 * half + (i >> 2)) * VP + (32 * t + 16 * (lane >> 4 & 1) + (i & 3) * 4) * 2;
-                        const uint2 one = attn_transposed(at), two = attn_transposed(at + 8 * VP);
-                        x = uint4v{one.x, one.y, two.x, two.y};
-                    } else {
-                        const int d = 32 * t + c;
-                        x = *reinterpret_cast<const uint4v*>(vb + d * 128 + ((2 * g + half) ^ attn_unit(d)) * 16);
-                    }
-                    if (apart) {
-                        constexpr unsigned EXP = BF ? 0x7f80u : 0x7c00u;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if ((x[j] & EXP) == EXP) x[j] &= 0xffff0000u;
-                            if ((x[j] >> 16 & EXP) == EXP) x[j] &= 0xffffu;
-                        }
-                    }
-                    o[t] = attn_mma32<BF>(x, w[g], o[t]);
-                }
         }
-        if (v + 1 < v_end) store(v + 1);
-    }
 
     const float2v both = attn_pair32(l);
     l = both[0] + both[1];
     if (!works || query >= seq.nq) return;
     if (seq.bad) l = __builtin_nanf("");
+    const int64_t token = seq.t0 + query;
     if (a.splits == 1) {
         const float f = p < 0 ? 0 : 1 / l;
         uint16_t* dst = a.out + ((int64_t)head * D + 4 * half) * a.ldo + token;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                dst[(int64_t)(32 * t + 8 * (i >> 2) + (i & 3)) * a.ldo] = attn_narrow<BF>(o[t][i] * f);
+            for (int i = 0; i < 16; ++i) dst[(int64_t)(32 * t + 8 * (i >> 2) + (i & 3)) * a.ldo] = attn_narrow<BF>(o[t][i] * f);
     } else {
         const int64_t at = ((int64_t)split * a.heads * a.group + head) * a.tokens + token;
 #pragma unroll

@@ -15,6 +15,13 @@ int64_t keys_seen(int64_t max_length, int window, int sinks, int64_t queries)
     return std::min<int64_t>(max_length, (int64_t)window + sinks + queries);
 }
 
+// Wavefronts of the tile kernel's workgroups: 8 share what they bring to the LDS, 4 where that leaves CUs without work
+void tile_shape(AttnPlan& p, int64_t items, int64_t pairs)
+{
+    p.waves = ceil_div(items, 8) * pairs >= 256 ? 8 : 4;
+    p.col_blocks = (int)ceil_div(items, p.waves);
+}
+
 }  // namespace
 
 AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t tokens, int max_queries, int64_t max_length, int window, int sinks)
@@ -27,7 +34,8 @@ AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t to
         p.col_tiles = (int)ceil_div(columns, 16);
         p.col_blocks = 1;
     } else {
-        p.col_blocks = (int)ceil_div(ceil_div(max_queries, ATTN_TILE_QUERIES) * group, ATTN_WAVES);
+        const int64_t items = ceil_div(max_queries, ATTN_TILE_QUERIES) * group;
+        tile_shape(p, items, (int64_t)batch * heads);
     }
     const int64_t base = (int64_t)batch * heads * p.col_blocks;
     // tiles of the longest sequence: window and sinks each may begin inside a tile
@@ -44,7 +52,8 @@ AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t to
 AttnPlan plan_prompt(int sequences, int heads, int group, int64_t max_tokens)
 {
     AttnPlan p = {};
-    p.col_blocks = (int)ceil_div(ceil_div(max_tokens, ATTN_TILE_QUERIES) * group, ATTN_WAVES);
+    const int64_t items = ceil_div(max_tokens, ATTN_TILE_QUERIES) * group;
+    tile_shape(p, items, (int64_t)sequences * heads);
     p.splits = 1;
     p.split_tiles = INT32_MAX;
     p.groups = (int64_t)sequences * heads * p.col_blocks;
