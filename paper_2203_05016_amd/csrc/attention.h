@@ -59,6 +59,9 @@ struct AttnArgs {
     int col_blocks;           // blocks of columns of a sequence and key head
 };
 
+// Wavefronts per SIMD of the decoding kernel: as many as its registers allow without spilling
+SHFLBW_HD constexpr int decode_residency(int col_tiles, int D) { return col_tiles == 1 ? 4 : col_tiles == 2 && D < 128 ? 3 : col_tiles == 4 && D == 128 ? 1 : 2; }
+constexpr int ATTN_FEW_ROWS = 2048;      // rows of a join up to which a row has a workgroup
 constexpr int ATTN_DECODE_KEYS = 32;     // keys of a tile of the decoding kernel
 constexpr int ATTN_TILE_KEYS = 64;       // keys of a tile of the other
 constexpr int ATTN_TILE_QUERIES = 32;    // queries of an item there
@@ -67,7 +70,7 @@ constexpr int64_t ATTN_MAX_LD = 1 << 26;  // of a prompt's keys and values: 32 r
 struct AttnPlan {
     bool decode;              // the kernel for few queries
     int col_tiles;            // its 16-column tiles per wavefront
-    int waves;                // the other's wavefronts per workgroup
+    int waves;                // wavefronts per workgroup
     int col_blocks, splits, split_tiles;
     int64_t groups;           // workgroups
     int64_t workspace;        // bytes

@@ -109,6 +109,11 @@ __device__ __forceinline__ uint2 attn_transposed(attn_lds p)
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((attn_lds4)p));
 }
 
+// Tables that nothing writes while a kernel runs, read at addresses that a wavefront's lanes share: through the scalar cache, so that
+// the wait for an entry is not one for the vector loads in flight
+typedef const __attribute__((address_space(4))) int32_t* attn_table;
+__device__ __forceinline__ attn_table attn_scalar(const int32_t* p) { return (attn_table)(uintptr_t)p; }
+
 // One sequence of a call
 struct AttnSeq {
     int64_t t0;    // its first column of q
@@ -121,8 +126,8 @@ __device__ __forceinline__ AttnSeq attn_sequence(const AttnArgs& a, int b)
     AttnSeq s;
     int64_t t0 = CACHE ? b : 0, t1 = CACHE ? b + 1 : a.tokens;
     if (a.starts) {
-        t0 = a.starts[b];
-        t1 = a.starts[b + 1];
+        t0 = attn_scalar(a.starts)[b];
+        t1 = attn_scalar(a.starts)[b + 1];
     }
     t0 = t0 < 0 ? 0 : t0;
     t1 = t1 > a.tokens ? a.tokens : t1;
@@ -131,7 +136,7 @@ __device__ __forceinline__ AttnSeq attn_sequence(const AttnArgs& a, int b)
     s.bad = false;
     if constexpr (CACHE) {
         const int64_t most = (int64_t)a.table_width << a.page_shift;
-        const int len = a.lengths[b];
+        const int len = attn_scalar(a.lengths)[b];
         s.bad = len > most;
         s.len = s.bad ? (int)most : len < 0 ? 0 : len;
     } else {
@@ -165,119 +170,138 @@ __device__ __forceinline__ AttnTiles attn_tiles(int first, int last, int window,
 __device__ __forceinline__ bool attn_sees(int j, int p, int lo, int sinks) { return (unsigned)j <= (unsigned)p && p >= 0 && (j >= lo || j < sinks); }
 __device__ __forceinline__ int attn_window_start(int p, int window) { return p < window ? 0 : p - window + 1; }
 
+// The maximum that scores are taken off follows the true one only when that has grown by this many powers of two: rescaling the
+// accumulators is rare then, and weights stay below 2^ATTN_SLACK.
+constexpr float ATTN_SLACK = 8;
+// the largest of three, without the rewriting of signalling NaN that fmaxf comes with
+__device__ __forceinline__ float attn_max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 // ---- few queries over the cache
 //
-// A workgroup takes one sequence, key head and part of the keys, and up to 16 NT columns: a column is one query head
+// A workgroup takes one sequence, key head and part of the keys, and all of its up to 16 NT columns: a column is one query head
 // of the key head's group, of one query.  Its wavefronts take tiles of 32 keys in turn, each with its own maximum, sum
 // and accumulators, and join through the LDS at the end.  Bound by the cache's bytes: a value is read once, as four bits.
 // The keys' words unpack in the registers of the lane that hands them to the matrix instruction; the
 // values' words belong to one key each (they share its scale) where the second product wants eight keys of one
 // feature per lane, so they go through a tile of LDS that only this wavefront uses and come back by transposing reads.
-// Loads are one tile ahead, page numbers two.
+// Loads are two tiles ahead, page numbers three.
 template <bool BF, int D, int NT, int W>
-__global__ __launch_bounds__(64 * W) void attention_decode_kernel(AttnArgs a)
+__global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_decode_kernel(AttnArgs a)
 {
-    constexpr int S = D / 32, DT = D / 16;
+    constexpr int S = D / 32, DT = D / 16, C = 16 * NT;
     constexpr int VP = 2 * D + 32;                        // LDS pitch of a key's values: 8 rows x 32 bytes in 64 banks
     constexpr int OP = D + 4;                             // pitch of a column's sums, in floats
+    constexpr int QP = 2 * D + 16;                        // pitch of a column's query: 16 rows in different banks
     constexpr int SB = scale_bytes(D);
-    constexpr int V_BYTES = W * 32 * VP, O_BYTES = W * 16 * OP * 4, Q_BYTES = NT * 16 * D * 2;
+    constexpr int V_BYTES = W * 32 * VP, O_BYTES = W * 16 * OP * 4, Q_BYTES = C * QP;
     constexpr int BYTES = V_BYTES > O_BYTES ? (V_BYTES > Q_BYTES ? V_BYTES : Q_BYTES) : (O_BYTES > Q_BYTES ? O_BYTES : Q_BYTES);
     __shared__ __attribute__((aligned(16))) char smem[BYTES];
-    __shared__ float stat[W][16 * NT][2];
+    __shared__ float stat[W][C][2];
+    __shared__ int64_t where[C];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int quarter = lane >> 4, r = lane & 15;
-    const int split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
-    const int cb = rest % a.col_blocks, pair = rest / a.col_blocks;
+    const int split = blockIdx.x % a.splits, pair = blockIdx.x / a.splits;
     const int b = pair / a.heads, h = pair % a.heads;
 
     const AttnSeq seq = attn_sequence<true>(a, b);
-    const int col0 = cb * 16 * NT, cols = seq.nq * a.group;
-    if (col0 >= cols) return;
-    const int last_col = (cols < col0 + 16 * NT ? cols : col0 + 16 * NT) - 1;
-    const int p0 = seq.len - seq.nq;
-    const int p_first = p0 + col0 / a.group, p_last = p0 + last_col / a.group;
+    const int cols = (seq.nq < C / a.group ? seq.nq : C / a.group) * a.group;   // (max_queries of them have room)
+    if (cols == 0) return;
+    const int p_first = seq.len - seq.nq, p_last = p_first + (cols - 1) / a.group;
     const AttnTiles tiles = attn_tiles(p_first, p_last, a.window, a.sinks, 0, ATTN_DECODE_KEYS);
     const int v_begin = split * a.split_tiles;
     const int v_end = tiles.count - v_begin < a.split_tiles ? tiles.count : v_begin + a.split_tiles;
 
     const int page = 1 << a.page_shift;
-    const int64_t chunk = page_head_bytes(page, D);
-    const int32_t* table = a.table + (int64_t)b * a.table_ld;
+    const int64_t chunk = page_head_bytes(page, D), page_bytes = chunk * a.heads;
+    const char* pages = a.cache + h * chunk;
+    const attn_table table = attn_scalar(a.table + (int64_t)b * a.table_ld);
+    const int v_row = ((lane >> 4) & 1) * 8 + ((lane >> 1) & 7), v_part = (lane & 1) + 2 * (lane >> 5);   // of the values' words (value_lane)
 
     struct Raw {
         unsigned k[2][S], v[2][S], ks[2], vs[2];
+        bool known;                                       // there is such a page
     };
     // page of tile v; tiles past the end read what the last one does
-    auto page_of = [&](int v) __attribute__((always_inline)) {
-        const int c = v < v_end ? v : v_end - 1;
-        return table[tiles.real(c) * ATTN_DECODE_KEYS >> a.page_shift];
+    const auto page_of = [&](int v) __attribute__((always_inline)) {
+        return table[tiles.real(v < v_end ? v : v_end - 1) * ATTN_DECODE_KEYS >> a.page_shift];
     };
-    auto load = [&](int v, int id) __attribute__((always_inline)) {
-        Raw x;
+    const auto load = [&](Raw& x, int v, int id) __attribute__((always_inline)) {
         const bool known = (unsigned)id < (unsigned)a.pages;
-        const int at = tiles.real(v) * ATTN_DECODE_KEYS & (page - 1);
-        const char* base = a.cache + ((int64_t)(known ? id : 0) * a.heads + h) * chunk;
-        const char* codes = base + code_offset(D, at, lane);
+        const int at = tiles.real(v < v_end ? v : v_end - 1) * ATTN_DECODE_KEYS & (page - 1);
+        const char* base = pages + (known ? id : 0) * page_bytes;
+        const char* codes = base + code_offset(D, at, 0);
+        const unsigned code_lane = D == 64 ? lane * 16 : lane * (D / 8);
 #pragma unroll
-        for (int kind = 0; kind < 2; ++kind, codes += page * D / 2) {
+        for (int kind = 0; kind < 2; ++kind, codes += page * (D / 2)) {
             unsigned(&w)[2][S] = kind ? x.v : x.k;
             if constexpr (D == 64) {
-                const uint4v t = *reinterpret_cast<const uint4v*>(codes);
+                const uint4v t = *reinterpret_cast<const uint4v*>(codes + code_lane);
                 w[0][0] = t[0]; w[0][1] = t[1]; w[1][0] = t[2]; w[1][1] = t[3];
             } else {
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int s = 0; s < S; ++s) w[u][s] = reinterpret_cast<const unsigned*>(codes + u * D * 8)[s];
+                    for (int s = 0; s < S; ++s) w[u][s] = reinterpret_cast<const unsigned*>(codes + code_lane + u * D * 8)[s];
             }
         }
-        const char* scales = base + (int64_t)page * D;
-        const int vr = ((lane >> 4) & 1) * 8 + ((lane >> 1) & 7);
+        const char* ks = base + page * D + at * SB;
+        const char* vs = ks + page * SB;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const char* ks = scales + (at + 16 * u + r) * SB;
-            const char* vs = scales + (page + at + 16 * u + vr) * SB;
-            x.ks[u] = SB == 2 ? *reinterpret_cast<const uint16_t*>(ks) : *reinterpret_cast<const unsigned*>(ks);
-            x.vs[u] = SB == 2 ? *reinterpret_cast<const uint16_t*>(vs) : *reinterpret_cast<const unsigned*>(vs);
-            if (!known) x.ks[u] = x.vs[u] = 0xffffffffu;   // a page that is not there reads as NaN
+            const unsigned k_lane = (16 * u + r) * SB, v_lane = (16 * u + v_row) * SB;
+            x.ks[u] = SB == 2 ? *reinterpret_cast<const uint16_t*>(ks + k_lane) : *reinterpret_cast<const unsigned*>(ks + k_lane);
+            x.vs[u] = SB == 2 ? *reinterpret_cast<const uint16_t*>(vs + v_lane) : *reinterpret_cast<const unsigned*>(vs + v_lane);
         }
-        return x;
+        x.known = known;
     };
 
-    int v = v_begin + wave;
-    Raw raw = {};
+    // the first two tiles travel while the queries are fetched
+    Raw even = {}, odd = {};
     int id = 0;
-    if (v < v_end) {
-        raw = load(v, page_of(v));
-        id = page_of(v + W);
+    if (v_begin < v_end) {
+        const int id0 = page_of(v_begin + wave), id1 = page_of(v_begin + wave + W);
+        load(even, v_begin + wave, id0);
+        load(odd, v_begin + wave + W, id1);
+        id = page_of(v_begin + wave + 2 * W);
     }
 
-    // queries: through the LDS once, columns x features, then as operands in registers
+    // queries: through the LDS once, columns x features, then as operands in registers.  A lane fetches one column's; neighbouring
+    // lanes take neighbouring queries of a head, which share lines of memory.
     uint4v q[NT][S];
+    int p[NT], lo[NT];
     {
-        uint16_t* qs = reinterpret_cast<uint16_t*>(smem);
-        for (int e = threadIdx.x; e < NT * 16 * D; e += 64 * W) {
-            const int c = e % (16 * NT), f = e / (16 * NT);
-            const int col = col0 + c;
-            uint16_t x = 0;
-            if (col < cols) x = a.q[((int64_t)(h * a.group + col % a.group) * D + f) * a.ldq + seq.t0 + col / a.group];
-            qs[c * D + f] = x;
-        }
+        constexpr int CP = C == 48 ? 64 : C, FS = 64 / CP;    // lanes per feature, features at a time
+        const int n = lane & (CP - 1), f0 = wave * FS + lane / CP, queries = cols / a.group;   // (a whole number: up to C columns in all)
+        const bool real = n < cols;
+        const int g = real ? n / queries : 0, i = real ? n % queries : 0, c = real ? i * a.group + g : n;
+        const uint16_t* src = a.q + ((int64_t)(h * a.group + g) * D + f0) * a.ldq + seq.t0 + i;
+        uint16_t x[D / (W * FS)];
+#pragma unroll
+        for (int k = 0; k < D / (W * FS); ++k) x[k] = src[(int64_t)(k * W * FS) * a.ldq];
+        if (c < C)
+#pragma unroll
+            for (int k = 0; k < D / (W * FS); ++k) *reinterpret_cast<uint16_t*>(smem + c * QP + (f0 + k * W * FS) * 2) = real ? x[k] : 0;
+        // where a column's results go: head and token
+        if (wave == 0 && n < C) where[c] = a.splits == 1 ? (int64_t)(h * a.group + g) * D * a.ldo + seq.t0 + i
+                                                         : ((int64_t)split * a.heads * a.group + h * a.group + g) * a.tokens + seq.t0 + i;
         __syncthreads();
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int s = 0; s < S; ++s) q[n][s] = *reinterpret_cast<const uint4v*>(qs + (16 * n + r) * D + 32 * s + 8 * quarter);
+            for (int s = 0; s < S; ++s) q[n][s] = *reinterpret_cast<const uint4v*>(smem + (16 * n + r) * QP + (32 * s + 8 * quarter) * 2);
         __syncthreads();
-    }
-    int p[NT], lo[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int col = col0 + 16 * n + r;
-        p[n] = col < cols ? p0 + col / a.group : -1;
-        lo[n] = attn_window_start(p[n], a.window);
+        for (int n = 0; n < NT; ++n) {
+            const int col = 16 * n + r;
+            p[n] = col < cols ? p_first + col / a.group : -1;
+            lo[n] = attn_window_start(p[n], a.window);
+        }
     }
 
     float4v o[NT][DT] = {};
@@ -286,53 +310,36 @@ __global__ __launch_bounds__(64 * W) void attention_decode_kernel(AttnArgs a)
     for (int n = 0; n < NT; ++n) { m[n] = -FLT_MAX; l[n] = 0; }
 
     char* vt = smem + wave * 32 * VP;
-    const int vw = (((lane >> 4) & 1) * 8 + ((lane >> 1) & 7)) * VP + ((lane & 1) + 2 * (lane >> 5)) * 16;
+    char* vw = vt + v_row * VP + v_part * 16;
     const attn_lds vr = (attn_lds)vt + (4 * quarter + (r >> 2)) * VP + (r & 3) * 8;
+    const int window_last = attn_window_start(p_last, a.window);
 
-    for (; v < v_end; v += W) {
-        Raw next = raw;
-        if (v + W < v_end) {
-            next = load(v + W, id);
-            id = page_of(v + 2 * W);
-        }
+    bool special = false;
+    // whether not all columns see all 32 keys from j on
+    const auto is_masked = [&](int j) __attribute__((always_inline)) { return j + 31 > p_first || (j < window_last && j + 31 >= a.sinks); };
+    const auto work = [&](Raw& raw, int v) __attribute__((always_inline)) {
         const int j0 = tiles.real(v) * ATTN_DECODE_KEYS;
-        const bool masked = j0 + 31 > p_first || (j0 < attn_window_start(p_last, a.window) && j0 + 31 >= a.sinks);
-
-        // values of keys that only some columns see must not reach the others as 0 * NaN: such blocks become zeros
-        // here, and NaN where they are seen
-        if (masked) {
-            unsigned special[2] = {0, 0};
+        if (!raw.known)                                   // a page that is not there reads as NaN
+#pragma unroll
+            for (int u = 0; u < 2; ++u) raw.ks[u] = raw.vs[u] = 0xffffffffu;
+        const bool masked = is_masked(j0);
+        // values of keys that only some columns see must not reach the others as 0 * NaN: such blocks are zeros here,
+        // and become NaN at the end where they are seen
+        if (masked)
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int s = 0; s < S; ++s)
                     if ((raw.vs[u] >> 8 * s & 255) == 255) {
-                        special[u] |= 1u << s;
+                        special = true;
                         raw.vs[u] &= ~(255u << 8 * s);
                         raw.v[u][s] = 0;
                     }
-            if (__any(special[0] | special[1])) {
-                for (int u = 0; u < 2; ++u)
-                    for (int i = 0; i < 16; ++i) {
-                        const int from = (i >> 3) * 16 + (i & 7) * 2;   // the first lane that holds this key
-                        const unsigned which = __builtin_amdgcn_readlane(u ? special[1] : special[0], from);
-                        if (!which) continue;
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            if (attn_sees(j0 + 16 * u + i, p[n], lo[n], a.sinks))
-#pragma unroll
-                                for (int t = 0; t < DT; ++t)
-                                    if (which >> (t / 2) & 1) o[n][t] += __builtin_nanf("");
-                    }
-            }
-        }
 
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int s = 0; s < S; ++s)
-                *reinterpret_cast<uint4v*>(vt + vw + 16 * u * VP + s * 64) = attn_unpack<BF>(raw.v[u][s], raw.vs[u] >> 8 * s & 255);
-
+            for (int s = 0; s < S; ++s) *reinterpret_cast<uint4v*>(vw + 16 * u * VP + s * 64) = attn_unpack<BF>(raw.v[u][s], raw.vs[u] >> 8 * s & 255);
         float4v sc[NT][2] = {};
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -342,34 +349,41 @@ __global__ __launch_bounds__(64 * W) void attention_decode_kernel(AttnArgs a)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) sc[n][u] = attn_mma16<BF>(k, q[n][s], sc[n][u]);
             }
+        load(raw, v + 2 * W, id);
+        id = page_of(v + 3 * W);
 
         uint4v w[NT];
+        if (masked)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (!attn_sees(j0 + (i >> 2) * 16 + quarter * 4 + (i & 3), p[n], lo[n], a.sinks)) sc[n][i >> 2][i & 3] = -INFINITY;
+        float top[NT];
+        bool grown = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float x[8], top = -INFINITY;
+            const float4v x = sc[n][0], y = sc[n][1];
+            top[n] = attn_max3(attn_max3(x[0], x[1], x[2]), attn_max3(x[3], y[0], y[1]), attn_max3(y[2], y[3], y[3])) * a.scale;
+            grown |= top[n] > m[n] + ATTN_SLACK;
+        }
+        if (__any(grown))
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] = sc[n][i >> 2][i & 3] * a.scale;
-                if (masked && !attn_sees(j0 + (i >> 2) * 16 + quarter * 4 + (i & 3), p[n], lo[n], a.sinks)) x[i] = -INFINITY;
-                top = fmaxf(top, x[i]);
-            }
-            float2v t = attn_pair16(top);
-            t = attn_pair32(fmaxf(t[0], t[1]));
-            top = fmaxf(t[0], t[1]);
-            if (__any(top > m[n])) {
-                const float now = fmaxf(m[n], top), shrink = attn_exp2(m[n] - now);
+            for (int n = 0; n < NT; ++n) {
+                float2v t = attn_pair16(top[n]);
+                t = attn_pair32(attn_max3(t[0], t[1], t[1]));
+                const float now = attn_max3(t[0], t[1], m[n]), shrink = attn_exp2(m[n] - now);
                 m[n] = now;
                 l[n] *= shrink;
 #pragma unroll
-                for (int t2 = 0; t2 < DT; ++t2) o[n][t2] *= shrink;
+                for (int d = 0; d < DT; ++d) o[n][d] *= shrink;
             }
-            float sum = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] = attn_exp2(x[i] - m[n]);
-                sum += x[i];
-            }
-            l[n] += sum;
+        for (int n = 0; n < NT; ++n) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = attn_exp2(__builtin_fmaf(sc[n][i >> 2][i & 3], a.scale, -m[n]));
+            l[n] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[n][i] = attn_pack<BF>(x[2 * i], x[2 * i + 1]);
         }
@@ -377,16 +391,38 @@ __global__ __launch_bounds__(64 * W) void attention_decode_kernel(AttnArgs a)
         asm volatile("" ::: "memory");
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
-            const uint2 first = attn_transposed(vr + t * 32), second = attn_transposed(vr + 16 * VP + t * 32);
-            const uint4v x = {first.x, first.y, second.x, second.y};
+            const uint2 one = attn_transposed(vr + t * 32), two = attn_transposed(vr + 16 * VP + t * 32);
+            const uint4v x = {one.x, one.y, two.x, two.y};
 #pragma unroll
             for (int n = 0; n < NT; ++n) o[n][t] = attn_mma16<BF>(x, w[n], o[n][t]);
         }
         asm volatile("" ::: "memory");
-        raw = next;
+    };
+    for (int v = v_begin + wave; v < v_end; v += W) {
+        work(even, v);
+        v += W;
+        if (v >= v_end) break;
+        work(odd, v);
     }
 
-    // join the wavefronts
+    if (__any(special))
+        for (int v = v_begin + wave; v < v_end; v += W) {
+            const int j0 = tiles.real(v) * ATTN_DECODE_KEYS;
+            if (!is_masked(j0)) continue;
+            for (int j = j0; j < j0 + ATTN_DECODE_KEYS && j <= p_last; ++j) {
+                const int page_j = table[j >> a.page_shift];
+                const bool there = (unsigned)page_j < (unsigned)a.pages;
+                const char* scales = pages + (there ? page_j : 0) * page_bytes + (int64_t)page * D + (int64_t)(page + (j & (page - 1))) * SB;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    if (attn_sees(j, p[n], lo[n], a.sinks))
+#pragma unroll
+                        for (int t = 0; t < DT; ++t)
+                            if (!there || (unsigned char)scales[t / 2] == 255) o[n][t] += __builtin_nanf("");
+            }
+        }
+
+    // join the wavefronts: every lane knows its column's maximum and sum over all of them
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         float2v t = attn_pair16(l[n]);
@@ -401,35 +437,34 @@ __global__ __launch_bounds__(64 * W) void attention_decode_kernel(AttnArgs a)
     float* sums = reinterpret_cast<float*>(smem);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        float top = -FLT_MAX;
+        const int col = 16 * n + r;
+        if (16 * n >= cols) break;
+        float top = -FLT_MAX, total = 0;
 #pragma unroll
-        for (int i = 0; i < W; ++i) top = fmaxf(top, stat[i][16 * n + r][0]);
-        const float f = attn_exp2(m[n] - top);
+        for (int i = 0; i < W; ++i) top = fmaxf(top, stat[i][col][0]);
+#pragma unroll
+        for (int i = 0; i < W; ++i) total += stat[i][col][1] * attn_exp2(stat[i][col][0] - top);
+        if (seq.bad) total = __builtin_nanf("");
+        float f = attn_exp2(m[n] - top);
+        if (a.splits == 1) f = p[n] < 0 ? 0 : f / total;
+        else if (seq.bad) f = total;
+        if (a.splits > 1 && wave == 0 && quarter == 0 && col < cols) {
+            const int64_t row = where[col];
+            a.part_ml[2 * row] = p[n] < 0 ? -INFINITY : top;
+            a.part_ml[2 * row + 1] = total;
+        }
 #pragma unroll
         for (int t = 0; t < DT; ++t) *reinterpret_cast<float4v*>(sums + (wave * 16 + r) * OP + 16 * t + 4 * quarter) = o[n][t] * f;
         __syncthreads();
-        for (int e = threadIdx.x; e < 16 * D; e += 64 * W) {
-            const int c = e / D, d = e % D, col = col0 + 16 * n + c;
-            if (col >= cols) continue;
-            float most = -FLT_MAX, total = 0, x = 0;
-            for (int i = 0; i < W; ++i) most = fmaxf(most, stat[i][16 * n + c][0]);
-            for (int i = 0; i < W; ++i) {
-                total += stat[i][16 * n + c][1] * attn_exp2(stat[i][16 * n + c][0] - most);
-                x += sums[(i * 16 + c) * OP + d];
-            }
-            const int pos = p0 + col / a.group, head = h * a.group + col % a.group;
-            const int64_t token = seq.t0 + col / a.group;
-            if (seq.bad) x = total = __builtin_nanf("");
-            if (a.splits == 1) {
-                a.out[((int64_t)head * D + d) * a.ldo + token] = attn_narrow<BF>(pos < 0 ? 0 : x / total);
-            } else {
-                const int64_t row = ((int64_t)split * a.heads * a.group + head) * a.tokens + token;
-                a.part_o[row * D + d] = x;
-                if (d == 0) {
-                    a.part_ml[2 * row] = pos < 0 ? -INFINITY : most;
-                    a.part_ml[2 * row + 1] = total;
-                }
-            }
+#pragma unroll
+        for (int k = 0; k < 16 * D / (64 * W); ++k) {
+            const int e = threadIdx.x + k * 64 * W, c = e / D, d = e % D, at = 16 * n + c;
+            if (at >= cols) break;
+            float x = 0;
+#pragma unroll
+            for (int i = 0; i < W; ++i) x += sums[(i * 16 + c) * OP + d];
+            if (a.splits == 1) a.out[where[at] + d * a.ldo] = attn_narrow<BF>(x);
+            else a.part_o[where[at] * D + d] = x;
         }
         __syncthreads();
     }
@@ -446,12 +481,10 @@ __global__ __launch_bounds__(64 * W) void attention_decode_kernel(AttnArgs a)
 //
 // A wavefront works on 32 keys at a time, three of them at once: the scores of the next, the softmax of this one, the second product
 // of the one before.  Matrix and vector instructions of such a step do not depend on each other, so that one wavefront issues
-// the latter while the former run.  The maximum that scores are taken off follows the true one only when that has grown by
-// ATTN_SLACK powers of two: rescaling the accumulators is rare then, and weights stay below 2^ATTN_SLACK.
+// the latter while the former run. 
 //
 // Infinities and NaN among the values of a tile that not all of the workgroup's queries see whole are zeros in the LDS, so that
 // they do not reach a query that does not see them as 0 * NaN; if there were any, they are added where they are seen at the end.
-constexpr float ATTN_SLACK = 8;
 constexpr int ATTN_AHEAD = 2;              // an operand is read this many steps of the reduction before its product
 
 template <bool BF, int D, bool CACHE>
@@ -467,14 +500,6 @@ struct AttnStage {
 // 16-byte unit u of a row of 64 tokens lies at unit u ^ attn_unit(row): the rows of 16 lanes' reads, and the 64-byte
 // pieces of four neighbouring rows, fall into different banks
 __device__ __forceinline__ int attn_unit(int row) { return ((row >> 1 & 1) << 2) | (row >> 2 & 1) << 1 | (row >> 3 & 1); }
-// the largest of three, without the rewriting of signalling NaN that fmaxf comes with
-__device__ __forceinline__ float attn_max3(float a, float b, float c)
-{
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
-
 template <bool BF, int D, bool CACHE, int W>
 __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
 {
@@ -545,7 +570,7 @@ __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
     const int page = 1 << a.page_shift;
     const int64_t chunk = page_head_bytes(page, D), page_bytes = chunk * a.heads;
     const char* pages = CACHE ? a.cache + h * chunk : nullptr;
-    const int32_t* table = CACHE ? a.table + (int64_t)b * a.table_ld : nullptr;
+    const attn_table table = attn_scalar(CACHE ? a.table + (int64_t)b * a.table_ld : nullptr);
     const int kind0 = W == 8 ? wave >> 2 : 0, brings = wave & 3, member = tid & 255;
     uint4v unit[KINDS][CACHE ? 1 : UNITS];
     unsigned word[KINDS][CACHE ? UNITS : 1], codes[KINDS] = {};
@@ -848,7 +873,7 @@ __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
             for (int k = from_key; k < from_key + ATTN_TILE_KEYS; ++k) {
                 if (!attn_sees(k, p, lo, a.sinks)) continue;
                 if constexpr (CACHE) {
-                    const int id = table[k >> a.page_shift];
+                    const int id = a.table[(int64_t)b * a.table_ld + (k >> a.page_shift)];
                     const bool there = (unsigned)id < (unsigned)a.pages;
                     const char* sc8 = pages + (there ? id : 0) * page_bytes + (int64_t)page * D + (int64_t)(page + (k & (page - 1))) * SB;
 #pragma unroll
@@ -895,31 +920,64 @@ __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
 
 // ---- join of the parts
 //
-// A workgroup takes 16 tokens of one query head: the parts' sums are read along their features, the results leave along the tokens.
-template <bool BF, int D>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a)
+// A wavefront takes one token of one query head, its lanes two features each, and reads the parts' sums along the features, all of
+// them at once; a workgroup's results leave along the tokens.  Where there are few rows, the parts of a row are shared by the
+// workgroup's four wavefronts instead.
+template <bool BF, int D, bool FEW>
+__global__ __launch_bounds__(FEW ? 256 : 1024) void attention_join_kernel(AttnArgs a)
 {
-    __shared__ uint16_t tile[D][17];
-    const int64_t token0 = (int64_t)blockIdx.x * 16;
-    const int head = blockIdx.y, heads = a.heads * a.group;
-    const int64_t stride = (int64_t)heads * a.tokens;
-    for (int e = threadIdx.x; e < 16 * D; e += 256) {
-        const int c = e / D, d = e % D;
-        if (token0 + c >= a.tokens) break;
+    constexpr int TOKENS = FEW ? 1 : 16;
+    __shared__ float tile[FEW ? 4 : TOKENS][D + 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t token0 = (int64_t)blockIdx.x * TOKENS;
+    const int head = blockIdx.y;
+    const int64_t stride = (int64_t)a.heads * a.group * a.tokens;
+    const bool has = 2 * lane < D;
+    const int c = FEW ? 0 : wave;
+    if (token0 + c < a.tokens) {
         const int64_t at = (int64_t)head * a.tokens + token0 + c;
-        float top = -FLT_MAX, total = 0, x = 0;
-        for (int i = 0; i < a.splits; ++i) top = fmaxf(top, a.part_ml[2 * (at + i * stride)]);
-        for (int i = 0; i < a.splits; ++i) {
-            const float f = attn_exp2(a.part_ml[2 * (at + i * stride)] - top);
-            total += a.part_ml[2 * (at + i * stride) + 1] * f;
-            x += a.part_o[(at + i * stride) * D + d] * f;
+        float top = -FLT_MAX, total = 0;
+        for (int i = 0; i < a.splits; i += 64) {
+            const int part = i + lane;
+            const float m = part < a.splits ? a.part_ml[2 * (at + part * stride)] : -FLT_MAX;
+            top = fmaxf(top, m);
         }
-        tile[d][c] = attn_narrow<BF>(a.part_ml[2 * at] == -INFINITY ? 0 : x / total);
+#pragma unroll
+        for (int by = 1; by < 64; by *= 2) top = fmaxf(top, __shfl_xor(top, by));
+        float2v x = {0, 0};
+        const bool none = a.part_ml[2 * at] == -INFINITY;
+#pragma unroll 8
+        for (int i = FEW ? wave : 0; i < a.splits; i += FEW ? 4 : 1) {
+            const float f = attn_exp2(a.part_ml[2 * (at + i * stride)] - top);
+            const float2v y = has ? *reinterpret_cast<const float2v*>(a.part_o + (at + i * stride) * D + 2 * lane) : float2v{0, 0};
+            total += a.part_ml[2 * (at + i * stride) + 1] * f;
+            x[0] += y[0] * f;
+            x[1] += y[1] * f;
+        }
+        if constexpr (FEW) {
+            if (has) {
+                tile[wave][2 * lane] = x[0];
+                tile[wave][2 * lane + 1] = x[1];
+            }
+            if (lane == 0) tile[wave][D] = total;
+            __syncthreads();
+            if (threadIdx.x < D) {
+                const int d = threadIdx.x;
+                const float y = (tile[0][d] + tile[1][d]) + (tile[2][d] + tile[3][d]), sum = (tile[0][D] + tile[1][D]) + (tile[2][D] + tile[3][D]);
+                a.out[((int64_t)head * D + d) * a.ldo + token0] = attn_narrow<BF>(none ? 0 : y / sum);
+            }
+        } else if (has) {
+            tile[c][2 * lane] = none ? 0 : x[0] / total;
+            tile[c][2 * lane + 1] = none ? 0 : x[1] / total;
+        }
     }
-    __syncthreads();
-    for (int e = threadIdx.x; e < 16 * D; e += 256) {
-        const int c = e & 15, d = e >> 4;
-        if (token0 + c < a.tokens) a.out[((int64_t)head * D + d) * a.ldo + token0 + c] = tile[d][c];
+    if constexpr (!FEW) {
+        __syncthreads();
+#pragma unroll
+        for (int e = threadIdx.x; e < TOKENS * D; e += 1024) {
+            const int c = e & 15, d = e >> 4;
+            if (token0 + c < a.tokens) a.out[((int64_t)head * D + d) * a.ldo + token0 + c] = attn_narrow<BF>(tile[c][d]);
+        }
     }
 }
 

@@ -6,6 +6,8 @@
 namespace shflbw {
 namespace {
 
+constexpr int CUS = 256;
+
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Keys that the queries of one workgroup see at most
@@ -18,7 +20,7 @@ int64_t keys_seen(int64_t max_length, int window, int sinks, int64_t queries)
 // Wavefronts of the tile kernel's workgroups: 8 share what they bring to the LDS, 4 where that leaves CUs without work
 void tile_shape(AttnPlan& p, int64_t items, int64_t pairs)
 {
-    p.waves = ceil_div(items, 8) * pairs >= 256 ? 8 : 4;
+    p.waves = ceil_div(items, 8) * pairs >= CUS ? 8 : 4;
     p.col_blocks = (int)ceil_div(items, p.waves);
 }
 
@@ -27,21 +29,32 @@ void tile_shape(AttnPlan& p, int64_t items, int64_t pairs)
 AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t tokens, int max_queries, int64_t max_length, int window, int sinks)
 {
     AttnPlan p = {};
-    const int64_t columns = (int64_t)group * max_queries;
+    const int64_t pairs = (int64_t)batch * heads, columns = (int64_t)group * max_queries;
     p.decode = columns <= 64;
-    const int tile = p.decode ? ATTN_DECODE_KEYS : ATTN_TILE_KEYS;
+    int64_t slots, least;   // workgroups the GPU holds at a time, and tiles that a part is worth
     if (p.decode) {
         p.col_tiles = (int)ceil_div(columns, 16);
         p.col_blocks = 1;
+        // Workgroups of 8 wavefronts while all of them are on the GPU at a time, of 4 beyond: 64 sequences of 2500 keys on average, 8 heads
+        // of 128: 40 us with 8, 44 with 4; 128 of 1028, 16 heads of 64: 35 and 29.
+        const int residency = decode_residency(p.col_tiles, D);
+        p.waves = residency >= 2 && pairs <= CUS * (residency / 2) ? 8 : 4;
+        slots = p.waves == 8 ? CUS * (residency / 2) : CUS * residency;
+        least = 4 * p.waves;
     } else {
-        const int64_t items = ceil_div(max_queries, ATTN_TILE_QUERIES) * group;
-        tile_shape(p, items, (int64_t)batch * heads);
+        tile_shape(p, ceil_div(max_queries, ATTN_TILE_QUERIES) * group, pairs);
+        slots = p.waves == 8 ? CUS : 2 * CUS;
+        least = 8;
     }
-    const int64_t base = (int64_t)batch * heads * p.col_blocks;
+    const int tile = p.decode ? ATTN_DECODE_KEYS : ATTN_TILE_KEYS;
+    const int64_t base = pairs * p.col_blocks;
     // tiles of the longest sequence: window and sinks each may begin inside a tile
     const int64_t tiles = keys_seen(max_length, window, sinks, max_queries) / tile + 3;
-    // enough workgroups for two on each of 256 CUs, but no part under 8 tiles (decoding: one per wavefront)
-    int64_t splits = std::min(ceil_div(512, std::max<int64_t>(base, 1)), std::max<int64_t>(tiles / 8, 1));
+    // Keys are cut into parts where workgroups are few, into as many as fill the GPU once (what is left over costs a whole round: 24
+    // sequences of 3000 keys, 8 heads of 128, 5 queries of 64 heads 48 us in 3 parts of 4 wavefronts, 41 in 2).  The join takes 4
+    // to 5 us, so parts are not worth it under twice their least length.
+    int64_t splits = base > 0 && tiles >= 2 * least ? std::min(slots / base, tiles / least) : 1;
+    splits = std::max<int64_t>(splits, 1);
     p.split_tiles = (int)ceil_div(tiles, splits);
     p.splits = (int)ceil_div(tiles, p.split_tiles);
     p.groups = base * p.splits;
