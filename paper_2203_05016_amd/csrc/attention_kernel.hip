@@ -173,13 +173,8 @@ __device__ __forceinline__ int attn_window_start(int p, int window) { return p <
 // The maximum that scores are taken off follows the true one only when that has grown by this many powers of two: rescaling the
 // accumulators is rare then, and weights stay below 2^ATTN_SLACK.
 constexpr float ATTN_SLACK = 8;
-// the largest of three, without the rewriting of signalling NaN that fmaxf comes with
-__device__ __forceinline__ float attn_max3(float a, float b, float c)
-{
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
+// (not in assembly: matrix results need wait states before a vector instruction reads them, which the compiler puts in)
+__device__ __forceinline__ float attn_max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
 // ---- few queries over the cache
 //

@@ -195,6 +195,23 @@ def test_prompt_values_that_are_not_finite(dtype):
                 check(got[:, at:at + n], *attend(*part, D, 0, dtype, window=window, sinks=sinks), "%d window %d" % (place, window))
 
 
+@pytest.mark.parametrize("counts", [None, [4, 3], [9, 6], [24, 30], [70, 40]])
+def test_the_same_bits_again(counts):
+    """Ten calls with the same arguments, masked and not: what a wait state or a barrier left out would show."""
+    for dtype, D in ((torch.float16, 64), (torch.bfloat16, 128)):
+        announce("the same bits", counts, dtype, D)
+        s = Served([1200, 700], 2, D, 64, dtype, seed=11)
+        q = _tensor(4 * D, sum(counts) if counts else 2, dtype, 59)
+        for mask in (dict(), dict(window=300, sinks=3)):
+            first = s.run(q, counts, **mask)
+            for _ in range(10):
+                assert torch.equal(first, s.run(q, counts, **mask))
+    prompt = [_tensor(4 * 64, 500, torch.float16, 61 + i, 0.3).to(DEV) for i in range(3)]
+    first = binding.window_attention(*prompt, 64, window=100, sinks=5)
+    for _ in range(10):
+        assert torch.equal(first, binding.window_attention(*prompt, 64, window=100, sinks=5))
+
+
 def test_large_and_small_scores():
     """Scores whose exponentials leave 32 bits, all equal scores, and rows of zeros."""
     dtype, D, n = torch.float16, 64, 100
