@@ -145,6 +145,8 @@ def _load_calls():
     address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
     m.connect(address(L.shflbw_spmm), address(L.shflbw_conv2d), address(L.shflbw_layernorm_transpose),
               torch._C._cuda_getCurrentRawStream)
+    m.connect_attention(address(L.shflbw_kv_write), address(L.shflbw_kv_read), address(L.shflbw_kv_attention_workspace),
+                        address(L.shflbw_kv_attention), address(L.shflbw_window_attention))
     return m
 
 
@@ -459,6 +461,8 @@ class KVCache:
     ``page * page_tokens + place`` holds one token; which pages a sequence has is the caller's bookkeeping.
     The memory is this object's: one torch uint8 tensor, zeros at first."""
 
+    _plan = None   # what the native calls need to know of the cache
+
     def __init__(self, pages, page_tokens, heads, head_dim, dtype, device="cuda:0"):
         import torch
         if dtype not in (torch.float16, torch.bfloat16):
@@ -470,7 +474,11 @@ class KVCache:
                              "head_dim 64, 96 or 128 (got %d pages of %d, %d heads of %d)" % (pages, page_tokens, heads, head_dim))
         self.pages, self.page_tokens, self.heads, self.head_dim, self.dtype = pages, page_tokens, heads, head_dim, dtype
         self._dev = torch.zeros(size, dtype=torch.uint8, device=device)
-        self._c = _Cache(self._dev.data_ptr(), pages, page_tokens, heads, head_dim, BF16 if dtype == torch.bfloat16 else F16)
+        bf16 = dtype == torch.bfloat16
+        self._c = _Cache(self._dev.data_ptr(), pages, page_tokens, heads, head_dim, BF16 if bf16 else F16)
+        native = calls()
+        if native and self._dev.is_cuda:
+            self._plan = native.cache_plan(self._dev.data_ptr(), pages, page_tokens, heads, head_dim, bf16, self._dev.device.index)
 
     @property
     def device(self):
@@ -481,6 +489,11 @@ class KVCache:
 
     def write(self, k, v, slots, stream=None):
         """Quantises column t of k and v into slot ``slots[t]`` (int32, on the GPU); slots outside the cache are skipped."""
+        if stream is None and self._plan is not None:
+            rc = _calls.kv_write(self._plan, k, v, slots)   # None: not the plain case, all checks below
+            if rc is not None:
+                _check(rc)
+                return
         rows = self.heads * self.head_dim
         ldk = _columns(k, "k", rows, self.dtype)
         ldv = _columns(v, "v", rows, self.dtype, k.shape[1])
@@ -491,6 +504,12 @@ class KVCache:
 
     def read(self, slots, k=None, v=None, stream=None):
         """(k, v) of the slots, (heads * head_dim, len(slots)) each; NaN for slots outside the cache."""
+        if k is None and v is None and stream is None and self._plan is not None:
+            both = _calls.kv_read(self._plan, slots)
+            if both is not None:
+                if type(both) is int:
+                    _check(both)
+                return both
         import torch
         n, rows = slots.shape[0] if slots.dim() else 0, self.heads * self.head_dim
         _indices(slots, "slots", n)
@@ -508,6 +527,12 @@ class KVCache:
         lengths (batch,) int32: its tokens in the cache.  max_queries and max_length: at least what any sequence has
         (max_length: all of the table's pages by default).  window 0 is none; the first ``sinks`` tokens stay visible
         past it.  What is on the GPU is not looked at by the host: see shflbw_kv_sequences for what bad entries do."""
+        if stream is None and self._plan is not None:
+            r = _calls.kv_attention(self._plan, q, table, lengths, starts, max_queries, max_length, window, sinks, out)
+            if r is not None:
+                if type(r) is int:
+                    _check(r)
+                return r if out is None else out
         import torch
         if q.dtype != self.dtype or q.dim() != 2 or q.shape[0] == 0 or q.shape[0] % (self.heads * self.head_dim):
             raise TypeError("q must be a 2-D %s tensor with a multiple of %d rows" % (self.dtype, self.heads * self.head_dim))
@@ -549,6 +574,12 @@ def window_attention(q, k, v, head_dim, starts=None, max_tokens=None, window=0, 
     Sequence b is columns ``starts[b]`` to ``starts[b + 1] - 1`` (int32, on the GPU); without starts all columns are one.
     max_tokens: at least the longest sequence's tokens (all of them by default).  A key at j is visible from p if
     j <= p and (window 0, or p - j < window, or j < sinks)."""
+    if stream is None and (_calls or calls()):
+        r = _calls.window_attention(q, k, v, head_dim, starts, max_tokens, window, sinks, out)   # None: not the plain case
+        if r is not None:
+            if type(r) is int:
+                _check(r)
+            return r if out is None else out
     import torch
     if q.dtype not in (torch.float16, torch.bfloat16) or q.dim() != 2 or k.dim() != 2:
         raise TypeError("q, k and v must be 2-D float16 or bfloat16 tensors")
