@@ -178,8 +178,8 @@ __device__ __forceinline__ float attn_max3(float a, float b, float c) { return f
 
 // ---- few queries over the cache
 //
-// A workgroup takes one sequence, key head and part of the keys, and all of its up to 16 NT columns: a column is one query head
-// of the key head's group, of one query.  Its wavefronts take tiles of 32 keys in turn, each with its own maximum, sum
+// A workgroup takes one sequence, key head and part of the keys, and up to 16 NT columns: a column is one query head of the
+// key head's group, of one query.  Its wavefronts take tiles of 32 keys in turn, each with its own maximum, sum
 // and accumulators, and join through the LDS at the end.  Bound by the cache's bytes: a value is read once, as four bits.
 // The keys' words unpack in the registers of the lane that hands them to the matrix instruction; the
 // values' words belong to one key each (they share its scale) where the second product wants eight keys of one
@@ -201,13 +201,16 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int quarter = lane >> 4, r = lane & 15;
-    const int split = blockIdx.x % a.splits, pair = blockIdx.x / a.splits;
+    const int split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits, block = rest % a.col_blocks, pair = rest / a.col_blocks;
     const int b = pair / a.heads, h = pair % a.heads;
 
-    const AttnSeq seq = attn_sequence<true>(a, b);
-    const int cols = (seq.nq < C / a.group ? seq.nq : C / a.group) * a.group;   // (max_queries of them have room)
-    if (cols == 0) return;
-    const int p_first = seq.len - seq.nq, p_last = p_first + (cols - 1) / a.group;
+    // a block of columns is a whole number of queries
+    AttnSeq seq = attn_sequence<true>(a, b);
+    const int skipped = block * (C / a.group), left = seq.nq - skipped;
+    if (left <= 0) return;
+    const int cols = (left < C / a.group ? left : C / a.group) * a.group;
+    seq.t0 += skipped;
+    const int p_first = seq.len - left, p_last = p_first + (cols - 1) / a.group;
     const AttnTiles tiles = attn_tiles(p_first, p_last, a.window, a.sinks, 0, ATTN_DECODE_KEYS);
     const int v_begin = split * a.split_tiles;
     const int v_end = tiles.count - v_begin < a.split_tiles ? tiles.count : v_begin + a.split_tiles;
@@ -495,8 +498,9 @@ struct AttnStage {
 // 16-byte unit u of a row of 64 tokens lies at unit u ^ attn_unit(row): the rows of 16 lanes' reads, and the 64-byte
 // pieces of four neighbouring rows, fall into different banks
 __device__ __forceinline__ int attn_unit(int row) { return ((row >> 1 & 1) << 2) | (row >> 2 & 1) << 1 | (row >> 3 & 1); }
-template <bool BF, int D, bool CACHE, int W>
-__global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
+// TINY: a prompt of fewer than 64 columns in all, brought value by value.
+template <bool BF, int D, bool CACHE, int W, bool TINY = false>
+__global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention_tile_kernel(AttnArgs a)
 {
     using Stage = AttnStage<BF, D, CACHE>;
     constexpr int S = D / 16, DT = D / 32, KP = Stage::KP, VP = Stage::VP;
@@ -571,10 +575,10 @@ __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
     unsigned word[KINDS][CACHE ? UNITS : 1], codes[KINDS] = {};
     int page_id = -1;                                      // cache: of the wavefront's keys of the next tile to load
     bool known = false, known_before = false;              // whether there is such a page: of the tile just loaded, of the one before
+    int tiny_key = 0;                                      // TINY: the next tile's first key
     const char* from[KINDS];                               // of the next tile to load, the same for all lanes of a wavefront
     const char* scales_from[KINDS];
     int64_t row_step[KINDS];                               // prompt: bytes of 32 rows
-    int64_t left[KINDS];                                   // and from there to the last 16 bytes of the tensor, or much
     unsigned lane_off[KINDS], scale_off[KINDS];            // a lane's bytes past these
     int lds_off[KINDS];
 #pragma unroll
@@ -591,7 +595,6 @@ __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
             row_step[n] = 64 * ld;
             lane_off[n] = 2 * ((unsigned)f * (unsigned)ld + (member & 7) * 8);
             lds_off[n] = (kind ? Stage::K_BYTES : 0) + f * 128 + ((member & 7) ^ attn_unit(f)) * 16;
-            left[n] = INT64_MAX;
         }
     }
     const auto find_page = [&](int j) __attribute__((always_inline)) {
@@ -600,9 +603,10 @@ __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
             page_id = table[idx < a.table_width ? idx : a.table_width - 1];   // (keys past the last page are hidden)
         }
     };
-    // What lies past a row's last column (the next row, or what is between them) is brought as well and hidden.  Past the last row's
-    // nothing is read: there the last 8 values are read, and moved to their places before they go to the LDS.
-    const auto at_end = [&](int j) __attribute__((always_inline)) { return !CACHE && h == a.heads - 1 && seq.t0 + j + ATTN_TILE_KEYS > a.tokens; };
+    // The last columns of a prompt end a tile, not begin one: what would lie past them is taken from before, where the tile before has it
+    // already (and these are hidden).  Keys of the tile whose first key would be j begin at:
+    const int prompt_last = CACHE || TINY ? INT32_MAX : (int)(a.tokens - ATTN_TILE_KEYS - seq.t0);
+    const auto begins = [&](int j) __attribute__((always_inline)) { return j < prompt_last ? j : prompt_last; };
     // the tile whose keys are j and up; next: those of the tile after it
     const auto load_begin = [&](int j, int next) __attribute__((always_inline)) {
         if constexpr (CACHE) {
@@ -617,16 +621,10 @@ __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
             find_page(next);
         } else {
             const int64_t tile = seq.t0 + j;
+            tiny_key = j;
 #pragma unroll
             for (int n = 0; n < KINDS; ++n) from[n] = reinterpret_cast<const char*>((kind0 + n ? a.v : a.k) + (int64_t)h * D * (kind0 + n ? a.ldv : a.ldk) + tile);
-            if (at_end(j))
-#pragma unroll
-                for (int n = 0; n < KINDS; ++n) left[n] = 2 * (((int64_t)D - 1) * (kind0 + n ? a.ldv : a.ldk) + a.tokens - 8 - tile);
         }
-    };
-    const auto most = [&](int n, int u) __attribute__((always_inline)) {   // the last offset from unit u's rows on
-        const int64_t x = left[n] - u * row_step[n];
-        return x < 0xffffffffLL ? (unsigned)x : 0xffffffffu;
     };
     const auto load_part = [&](int i) __attribute__((always_inline)) {
         if constexpr (CACHE) {
@@ -638,29 +636,23 @@ __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
             codes[i] = SB == 2 ? *reinterpret_cast<const uint16_t*>(sc) : *reinterpret_cast<const unsigned*>(sc);
         } else {
             const int n = i / UNITS, u = i % UNITS;
-            const unsigned end = most(n, u), off = lane_off[n] < end ? lane_off[n] : end;
-            __builtin_memcpy(&unit[n][u], from[n] + u * row_step[n] + off, 16);
+            if constexpr (TINY) {
+                const int64_t at = seq.t0 + tiny_key + (member & 7) * 8;
+                uint4v x = {0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (at + k < a.tokens) x[k >> 1] |= (unsigned)reinterpret_cast<const uint16_t*>(from[n] + u * row_step[n] + lane_off[n])[k] << 16 * (k & 1);
+                unit[n][u] = x;
+            } else {
+                __builtin_memcpy(&unit[n][u], from[n] + u * row_step[n] + lane_off[n], 16);
+            }
         }
     };
-    const auto store_begin = [&](int j, bool clean) __attribute__((always_inline)) {
-        if constexpr (CACHE) {
+    const auto store_begin = [&](bool clean) __attribute__((always_inline)) {
+        if constexpr (CACHE)
             if (!known_before)                             // a page that is not there reads as NaN
 #pragma unroll
                 for (int n = 0; n < KINDS; ++n) codes[n] = 0xffffffffu;
-        } else if (at_end(j)) {
-#pragma unroll
-            for (int n = 0; n < KINDS; ++n)
-#pragma unroll
-                for (int i = 0; i < UNITS; ++i) {
-                    const unsigned end = most(n, i), by = lane_off[n] > end ? (lane_off[n] - end) / 2 : 0;
-                    uint64_t x = unit[n][i][0] | (uint64_t)unit[n][i][1] << 32, y = unit[n][i][2] | (uint64_t)unit[n][i][3] << 32;
-                    const int bits = (int)(by & 3) * 16;
-                    if (by >= 4) { x = y; y = 0; }
-                    if (bits) { x = x >> bits | y << (64 - bits); y >>= bits; }
-                    if (by >= 8) x = y = 0;
-                    unit[n][i] = uint4v{(unsigned)x, (unsigned)(x >> 32), (unsigned)y, (unsigned)(y >> 32)};
-                }
-        }
         if (!clean || kind0 + KINDS == 1) return;
         constexpr int n = KINDS - 1;
         bool found = false;
@@ -733,8 +725,9 @@ __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
     float m = -FLT_MAX, l = 0;
 
     // half SUB of a tile, keys j and up, whose scores are in sc[SUB]: its weights; beside it the other half's scores (of the
-    // next tile, where SUB is 1), the product of the weights before, and a part of the staging.  part: the tile is a partial one.
-    const auto step = [&](auto which, int j, bool part, int next_buf, int last_buf, int stage_buf, int j_before, int j_after) __attribute__((always_inline)) {
+    // next tile, where SUB is 1), the product of the weights before, and a part of the staging.  part: the tile is a partial one; keys
+    // below `hide` are another tile's.
+    const auto step = [&](auto which, int j, int hide, bool part, int next_buf, int last_buf, int stage_buf, int j_before, int j_after) __attribute__((always_inline)) {
         constexpr int SUB = decltype(which)::value;
         const auto stage = [&](int i) __attribute__((always_inline)) {
             if constexpr (SUB == 0) store_part(i, stage_buf);
@@ -748,11 +741,11 @@ __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
                 w[SUB][0] = w[SUB][1] = uint4v{};
                 return;
             }
-            if (is_masked(j))
+            if (is_masked(j) || (!CACHE && j < hide))
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int k = j + (CACHE ? 8 * (i >> 2) + 4 * half + (i & 3) : 16 * (i >> 3) + 8 * half + (i & 7));
-                    if (!attn_sees(k, p, lo, a.sinks)) sc[SUB][i] = -INFINITY;
+                    if (!attn_sees(k, p, lo, a.sinks) || (!CACHE && k < hide)) sc[SUB][i] = -INFINITY;
                 }
         }
         // Pieces of all that, in an order that keeps both units busy: per step of the reduction an operand of each product is
@@ -814,7 +807,8 @@ __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
     if (tid == 0) special = 0;
     // past the last tile that one is brought again, to a buffer that is not read any more
     const auto clamped = [&](int v) __attribute__((always_inline)) { return first_key(v < v_end ? v : v_end - 1); };
-    int j = clamped(v_begin), j_next = clamped(v_begin + 1);
+    int own = clamped(v_begin), own_next = clamped(v_begin + 1);       // the tiles' own keys ..
+    int j = begins(own), j_next = begins(own_next);                    // .. and what is brought
     if (v_begin < v_end) {
         find_page(j);
         load_begin(j, j_next);
@@ -824,10 +818,10 @@ __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
     }
     __syncthreads();
     if (v_begin < v_end) {
-        store_begin(j, partial(j));
+        store_begin(partial(j));
 #pragma unroll
         for (int i = 0; i < PARTS; ++i) store_part(i, 0);
-        load_begin(j_next, clamped(v_begin + 2));
+        load_begin(j_next, begins(clamped(v_begin + 2)));
 #pragma unroll
         for (int i = 0; i < PARTS; ++i) load_part(i);
         known_before = known;
@@ -837,20 +831,22 @@ __global__ __launch_bounds__(64 * W, 2) void attention_tile_kernel(AttnArgs a)
 #pragma unroll
         for (int s = 0; s < S; ++s) sc[0] = attn_mma32<BF>(key_operand(0, 0, s), q[s], sc[0]);
     int buf = 0, before = 2 * Stage::BYTES, j_before = INT32_MAX;
-    bool part = partial(j);
+    bool part = partial(j) || j != own;
     for (int v = v_begin; v < v_end; ++v) {
         const int after = buf == 2 * Stage::BYTES ? 0 : buf + Stage::BYTES;
-        const bool part_next = partial(j_next);
-        store_begin(j_next, part_next);
-        step(std::integral_constant<int, 0>{}, j, part, buf, before, after, j_before, j + 32);
+        const bool part_next = partial(j_next) || j_next != own_next;
+        store_begin(part_next);
+        step(std::integral_constant<int, 0>{}, j, own, part, buf, before, after, j_before, j + 32);
         __syncthreads();
-        const int j_then = clamped(v + 2);
+        const int own_then = clamped(v + 2), j_then = begins(own_then);
         load_begin(j_then, clamped(v + 3));
-        step(std::integral_constant<int, 1>{}, j + 32, part, after, buf, 0, j, j_next);
+        step(std::integral_constant<int, 1>{}, j + 32, own, part, after, buf, 0, j, j_next);
         known_before = known;
         j_before = j + 32;
         j = j_next;
         j_next = j_then;
+        own = own_next;
+        own_next = own_then;
         part = part_next;
         before = buf;
         buf = after;

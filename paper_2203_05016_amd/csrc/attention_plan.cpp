@@ -17,13 +17,6 @@ int64_t keys_seen(int64_t max_length, int window, int sinks, int64_t queries)
     return std::min<int64_t>(max_length, (int64_t)window + sinks + queries);
 }
 
-// Wavefronts of the tile kernel's workgroups: 8 share what they bring to the LDS, 4 where that leaves CUs without work
-void tile_shape(AttnPlan& p, int64_t items, int64_t pairs)
-{
-    p.waves = ceil_div(items, 8) * pairs >= CUS ? 8 : 4;
-    p.col_blocks = (int)ceil_div(items, p.waves);
-}
-
 }  // namespace
 
 AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t tokens, int max_queries, int64_t max_length, int window, int sinks)
@@ -35,15 +28,24 @@ AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t to
     if (p.decode) {
         p.col_tiles = (int)ceil_div(columns, 16);
         p.col_blocks = 1;
+        // 64 columns leave one wavefront per SIMD (D = 128): two blocks of 32, of whole queries, read the cache twice and are faster.  16
+        // sequences of 3000 keys on average, 8 queries of 64 heads over 8 of 128: 48 -> 35 us; 32 of them 66 -> 54; of 64 features
+        // 28 -> 24; but 24 of 2100, 5 queries, in 48 columns 34 and in two blocks 41.
+        if (p.col_tiles == 4 && group <= 32) {
+            p.col_tiles = 2;
+            p.col_blocks = (int)ceil_div(max_queries, 32 / group);
+        }
         // Workgroups of 8 wavefronts while all of them are on the GPU at a time, of 4 beyond: 64 sequences of 2500 keys on average, 8 heads
         // of 128: 40 us with 8, 44 with 4; 128 of 1028, 16 heads of 64: 35 and 29.
         const int residency = decode_residency(p.col_tiles, D);
-        p.waves = residency >= 2 && pairs <= CUS * (residency / 2) ? 8 : 4;
+        p.waves = residency > 1 && pairs * p.col_blocks <= CUS * (residency / 2) ? 8 : 4;
         slots = p.waves == 8 ? CUS * (residency / 2) : CUS * residency;
         least = 4 * p.waves;
     } else {
-        tile_shape(p, ceil_div(max_queries, ATTN_TILE_QUERIES) * group, pairs);
-        slots = p.waves == 8 ? CUS : 2 * CUS;
+        const int64_t items = ceil_div(max_queries, ATTN_TILE_QUERIES) * group;
+        p.waves = items > 4 ? 8 : 4;
+        p.col_blocks = (int)ceil_div(items, p.waves);
+        slots = p.waves == 4 && D < 128 ? 2 * CUS : CUS;   // what the LDS holds of three tiles
         least = 8;
     }
     const int tile = p.decode ? ATTN_DECODE_KEYS : ATTN_TILE_KEYS;
@@ -62,14 +64,16 @@ AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t to
     return p;
 }
 
-AttnPlan plan_prompt(int sequences, int heads, int group, int64_t max_tokens)
+AttnPlan plan_prompt(int sequences, int heads, int group, int D, int64_t max_tokens)
 {
     AttnPlan p = {};
-    const int64_t items = ceil_div(max_tokens, ATTN_TILE_QUERIES) * group;
-    tile_shape(p, items, (int64_t)sequences * heads);
+    const int64_t items = ceil_div(max_tokens, ATTN_TILE_QUERIES) * group, pairs = (int64_t)sequences * heads;
+    // Workgroups of 8 wavefronts share what they bring to the LDS; of 4 where 8 leave CUs without work, and for heads of 64 (tile_residency)
+    p.waves = D > 64 && ceil_div(items, 8) * pairs >= CUS ? 8 : 4;
+    p.col_blocks = (int)ceil_div(items, p.waves);
     p.splits = 1;
     p.split_tiles = INT32_MAX;
-    p.groups = (int64_t)sequences * heads * p.col_blocks;
+    p.groups = pairs * p.col_blocks;
     return p;
 }
 

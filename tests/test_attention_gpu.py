@@ -344,3 +344,30 @@ def test_offsets_past_32_bits():
         starts = torch.tensor([0, nq], dtype=torch.int32, device=DEV)
         got = cache.attention(q.to(DEV), table, torch.tensor([40], dtype=torch.int32, device=DEV), starts, nq)
         check(got, *attend(q.double().numpy(), kd, vd, 128, 40 - nq, dtype))
+
+
+@pytest.mark.parametrize("D,group,counts", [(128, 8, [8, 7, 1, 8]), (64, 5, [11, 12, 3, 10]), (96, 17, [3, 3, 1, 2]), (128, 33, [1, 1, 1, 1])])
+def test_columns_in_blocks(D, group, counts):
+    """More than 48 columns: blocks of whole queries, the last ones of them ragged, or not there."""
+    lengths = [300, 12, 64, 101]
+    s = Served(lengths, 1, D, 32, torch.bfloat16, seed=12)
+    q = _tensor(group * D, sum(counts), torch.bfloat16, 64)
+    for window, sinks in [(0, 0), (40, 3)]:
+        announce("blocks of columns", D, group, counts, window)
+        got = s.run(q, counts, window=window, sinks=sinks)
+        assert "decode_kernel<%d,%d columns" % (D, 48 if group == 33 else 32) in binding.last_kernel()
+        check(got, *s.want(q, counts, window=window, sinks=sinks), "window %d" % window)
+
+
+def test_prompts_around_a_tile():
+    """Prompts of 60 to 70 columns in all, whose last tile takes its columns from before, alone and after another."""
+    for D, tokens, cut in ((64, 63, 20), (64, 64, 63), (96, 65, 64), (128, 66, 1), (64, 127, 64), (128, 129, 100)):
+        announce("around a tile", D, tokens, cut)
+        q, k, v = (_tensor(n * D, tokens, torch.float16, 75 + i, 0.3) for i, n in enumerate((2, 1, 1)))
+        for bounds in ([0, tokens], [0, cut, tokens]):
+            starts = torch.tensor(bounds, dtype=torch.int32, device=DEV)
+            for window, sinks in [(0, 0), (10, 2)]:
+                got = binding.window_attention(q.to(DEV), k.to(DEV), v.to(DEV), D, starts, tokens, window, sinks)
+                for a, b in zip(bounds, bounds[1:]):
+                    part = [x[:, a:b].double().numpy() for x in (q, k, v)]
+                    check(got[:, a:b], *attend(*part, D, 0, torch.float16, window=window, sinks=sinks), "%r window %d" % (bounds, window))
