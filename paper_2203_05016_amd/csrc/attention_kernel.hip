@@ -498,6 +498,26 @@ struct AttnStage {
 // 16-byte unit u of a row of 64 tokens lies at unit u ^ attn_unit(row): the rows of 16 lanes' reads, and the 64-byte
 // pieces of four neighbouring rows, fall into different banks
 __device__ __forceinline__ int attn_unit(int row) { return ((row >> 1 & 1) << 2) | (row >> 2 & 1) << 1 | (row >> 3 & 1); }
+// Calls hide(i) for those of N scores, of keys from + key(i), that a query at position p does not see, or that lie below `least`.  Away from the
+// sinks one comparison tells: key(i) - (begin - from) as an unsigned number is at most p - begin.
+template <int N, class Key, class Hide>
+__device__ __forceinline__ void attn_hide(int from, int p, int lo, int least, int sinks, bool near_sinks, Key&& key, Hide&& hide)
+{
+    if (near_sinks) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (!attn_sees(from + key(i), p, lo, sinks) || from + key(i) < least) hide(i);
+        return;
+    }
+    const int begin = lo > least ? lo : least;
+    const bool none = p < begin;
+    const int offset = none ? 1 << 30 : begin - from;
+    const unsigned span = none ? 0 : p - begin;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if ((unsigned)(key(i) - offset) > span) hide(i);
+}
+
 // TINY: a prompt of fewer than 64 columns in all, brought value by value.
 template <bool BF, int D, bool CACHE, int W, bool TINY = false>
 __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention_tile_kernel(AttnArgs a)
@@ -742,11 +762,10 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
                 return;
             }
             if (is_masked(j) || (!CACHE && j < hide))
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int k = j + (CACHE ? 8 * (i >> 2) + 4 * half + (i & 3) : 16 * (i >> 3) + 8 * half + (i & 7));
-                    if (!attn_sees(k, p, lo, a.sinks) || (!CACHE && k < hide)) sc[SUB][i] = -INFINITY;
-                }
+                attn_hide<16>(
+                    j + (CACHE ? 4 : 8) * half, p, lo, CACHE ? 0 : hide, a.sinks, j < a.sinks,
+                    [](int i) __attribute__((always_inline)) { return CACHE ? 8 * (i >> 2) + (i & 3) : 16 * (i >> 3) + (i & 7); },
+                    [&](int i) __attribute__((always_inline)) { sc[SUB][i] = -INFINITY; });
         }
         // Pieces of all that, in an order that keeps both units busy: per step of the reduction an operand of each product is
         // read ATTN_AHEAD steps before its use, two products are issued, and a share of the vector work follows: the maximum, whether
