@@ -79,6 +79,23 @@ struct AttnPlan {
     int64_t workspace;        // bytes
 };
 
+// Which sequence and key head (pair), and which of its per_pair workgroups, workgroup `block` of the tile kernel is.  The GPU deals workgroups
+// to its eight XCDs in turn.  Where heads come in fours, a pair's workgroups are on one XCD, whose L2 holds its keys and values, and every XCD
+// has much the same share of each sequence: 8 prompts of 400 to 4000 tokens, 16 query heads of 128 over 4, 298 us, dealt to all XCDs 315.
+// Other pairs, and what eights of pairs leave over, are dealt to all XCDs alike: 16 over 2 heads of 4 such prompts 171 us, on one XCD each
+// 285; one prompt of 8000, 5 over 1 head, 166 and 870.
+struct AttnPlace {
+    int pair, inner;
+};
+SHFLBW_HD inline AttnPlace attn_place(int block, int pairs, int heads, int per_pair)
+{
+    const int dealt = heads % 4 ? pairs : pairs % 8, at = block - dealt * per_pair;
+    if (at >= 0) return AttnPlace{dealt + at % 8 + at / 8 / per_pair * 8, at / 8 % per_pair};
+    // round r begins on XCD dealt * r % 8, which comes back after 8 / (dealt's power of two) rounds: then all move on by one
+    const int round = block / dealt, two = dealt & -dealt, on = (int)((int64_t)round * (two < 8 ? two : 8) / 8 % dealt);
+    return AttnPlace{(block % dealt + on) % dealt, round};
+}
+
 // How attention over the cache is cut.  max_queries, max_length: of any sequence.
 AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t tokens, int max_queries, int64_t max_length, int window, int sinks);
 // The same for a prompt, which needs no workspace

@@ -533,20 +533,8 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5, c = lane & 31, r = lane & 15;
-    // Where heads come in fours, a sequence and key head's workgroups are on one XCD, whose L2 holds its keys and values, and every XCD has
-    // much the same share of each sequence: 8 prompts of 400 to 4000 tokens, 16 query heads of 128 over 4, 298 us, dealt to all XCDs 315.
-    // Other pairs, and what eights of pairs leave over, are dealt, one XCD further in every round where their number is even: 16 over 2
-    // heads of 4 such prompts 171 us, on one XCD each 285; one prompt of 8000, 5 over 1 head, 166 and 870.  Blocks with most keys first.
-    const int per_pair = a.col_blocks * a.splits, pairs = a.batch * a.heads, over = a.heads % 4 ? pairs : pairs % 8;
-    const int at = (int)blockIdx.x - over * per_pair;
-    int pair, inner;
-    if (at < 0) {
-        inner = (int)blockIdx.x / over;
-        pair = ((int)blockIdx.x % over + (over % 2 ? 0 : inner % over)) % over;
-    } else {
-        inner = at / 8 % per_pair;
-        pair = over + at % 8 + at / 8 / per_pair * 8;
-    }
+    const AttnPlace at = attn_place((int)blockIdx.x, a.batch * a.heads, a.heads, a.col_blocks * a.splits);
+    const int pair = at.pair, inner = at.inner;      // blocks with most keys first
     const int blk = a.col_blocks - 1 - inner / a.splits, split = inner % a.splits;
     const int b = pair / a.heads, h = pair % a.heads;
 
