@@ -518,7 +518,7 @@ __device__ __forceinline__ void attn_hide(int from, int p, int lo, int least, in
         if ((unsigned)(key(i) - offset) > span) hide(i);
 }
 
-// TINY: a prompt of fewer than 64 columns in all, brought value by value.
+// TINY: a prompt of fewer than 64 columns in all.
 template <bool BF, int D, bool CACHE, int W, bool TINY = false>
 __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention_tile_kernel(AttnArgs a)
 {
@@ -593,7 +593,6 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
     unsigned word[KINDS][CACHE ? UNITS : 1], codes[KINDS] = {};
     int page_id = -1;                                      // cache: of the wavefront's keys of the next tile to load
     bool known = false, known_before = false;              // whether there is such a page: of the tile just loaded, of the one before
-    int tiny_key = 0;                                      // TINY: the next tile's first key
     const char* from[KINDS];                               // of the next tile to load, the same for all lanes of a wavefront
     const char* scales_from[KINDS];
     int64_t row_step[KINDS];                               // prompt: bytes of 32 rows
@@ -639,7 +638,6 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
             find_page(next);
         } else {
             const int64_t tile = seq.t0 + j;
-            tiny_key = j;
 #pragma unroll
             for (int n = 0; n < KINDS; ++n) from[n] = reinterpret_cast<const char*>((kind0 + n ? a.v : a.k) + (int64_t)h * D * (kind0 + n ? a.ldv : a.ldk) + tile);
         }
@@ -655,12 +653,15 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
         } else {
             const int n = i / UNITS, u = i % UNITS;
             if constexpr (TINY) {
-                const int64_t at = seq.t0 + tiny_key + (member & 7) * 8;
-                uint4v x = {0, 0, 0, 0};
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (at + k < a.tokens) x[k >> 1] |= (unsigned)reinterpret_cast<const uint16_t*>(from[n] + u * row_step[n] + lane_off[n])[k] << 16 * (k & 1);
-                unit[n][u] = x;
+                // 16 bytes, whatever they hold past the last column (a NaN in there only costs time); what would end past the last
+                // row's last column is loaded further down and moved
+                const char* at = from[n] + u * row_step[n] + lane_off[n];
+                const char* last = reinterpret_cast<const char*>(kind0 + n ? a.v : a.k) + row_step[n] / 32 * ((int64_t)a.heads * D - 1) + 2 * (a.tokens - 8);
+                const int over = at > last ? (int)(at - last) : 0;
+                unsigned __int128 x;
+                __builtin_memcpy(&x, at - over, 16);
+                if (over) x = over < 16 ? x >> 8 * over : 0;
+                __builtin_memcpy(&unit[n][u], &x, 16);
             } else {
                 __builtin_memcpy(&unit[n][u], from[n] + u * row_step[n] + lane_off[n], 16);
             }

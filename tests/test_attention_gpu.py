@@ -371,3 +371,16 @@ def test_prompts_around_a_tile():
                 for a, b in zip(bounds, bounds[1:]):
                     part = [x[:, a:b].double().numpy() for x in (q, k, v)]
                     check(got[:, a:b], *attend(*part, D, 0, torch.float16, window=window, sinks=sinks), "%r window %d" % (bounds, window))
+
+
+@pytest.mark.parametrize("D", [64, 96, 128])
+def test_short_prompts_inside_wider_rows(D):
+    """Fewer than 64 columns, with NaN beside them in rows of other lengths, or rows that end where the memory does."""
+    for tokens, ld, at in ((1, 1, 0), (1, 9, 4), (7, 7, 0), (9, 9, 0), (33, 40, 7), (62, 62, 0), (63, 70, 3)):
+        announce("short prompt", D, tokens, ld, at)
+        bufs = [torch.full((n * D, ld), NAN, dtype=torch.bfloat16, device=DEV) for n in (4, 2, 2)]
+        q, k, v = (x[:, at:at + tokens] for x in bufs)
+        for i, x in enumerate((q, k, v)):
+            x.copy_(_tensor(x.shape[0], tokens, torch.bfloat16, 210 + i, 0.3))
+        got = binding.window_attention(q, k, v, D)
+        check(got, *attend(*[x.double().cpu().numpy() for x in (q, k, v)], D, 0, torch.bfloat16), "%d of %d" % (tokens, ld))
