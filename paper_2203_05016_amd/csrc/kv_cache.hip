@@ -2,7 +2,9 @@
 //
 // Activations are features x tokens, so a thread takes one token's 32 features of a block at the stride of a row, and
 // neighbouring threads take neighbouring tokens: every load and store of the 16-bit side is contiguous along the tokens.
-// Bound by memory: 2 bytes of a value in or out, 17/32 in the cache.
+// Bound by memory: 2 bytes of a value in or out, 17/32 in the cache (13/24 for heads of 96, whose scales are padded).  65536 tokens, 8 heads of
+// 128 (f16): 340 MB each way, 79 us to write and 82 to read, 4.2 TB/s; a large copy moves 5.1.  Two tokens a thread, with half as many and
+// wider accesses, took 192 us for both where one takes 162.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
