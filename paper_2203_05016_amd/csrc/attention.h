@@ -98,8 +98,8 @@ SHFLBW_HD inline AttnPlace attn_place(int block, int pairs, int heads, int per_p
 
 // How attention over the cache is cut.  max_queries, max_length: of any sequence.
 AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t tokens, int max_queries, int64_t max_length, int window, int sinks);
-// The same for a prompt, which needs no workspace
-AttnPlan plan_prompt(int sequences, int heads, int group, int D, int64_t max_tokens);
+// The same for prompts, which need no workspace
+AttnPlan plan_prompt(int sequences, int heads, int group, int D, int64_t max_tokens, int window, int sinks);
 
 // SHFLBW_OK, or why the cache cannot be used (host checks of its fields)
 int check_cache(const shflbw_kv_cache* cache);

@@ -15,9 +15,9 @@ extern "C" void probe_cache_plan(int batch, int heads, int group, int D, long to
 {
     put(plan_cache_attention(batch, heads, group, D, tokens, max_queries, max_length, window, sinks), out);
 }
-extern "C" void probe_prompt_plan(int sequences, int heads, int group, int D, long max_tokens, long* out)
+extern "C" void probe_prompt_plan(int sequences, int heads, int group, int D, long max_tokens, int window, int sinks, long* out)
 {
-    put(plan_prompt(sequences, heads, group, D, max_tokens), out);
+    put(plan_prompt(sequences, heads, group, D, max_tokens, window, sinks), out);
 }
 extern "C" int probe_place(int block, int pairs, int heads, int per_pair, int* inner)
 {

@@ -26,7 +26,7 @@ def probe(tmp_path_factory):
     i, l, p = ctypes.c_int, ctypes.c_long, ctypes.c_void_p
     L.probe_cache_plan.argtypes = [i, i, i, i, l, i, l, i, i, p]
     L.probe_cache_plan.restype = None
-    L.probe_prompt_plan.argtypes = [i, i, i, i, l, p]
+    L.probe_prompt_plan.argtypes = [i, i, i, i, l, i, i, p]
     L.probe_prompt_plan.restype = None
     L.probe_place.argtypes = [i, i, i, i, ctypes.POINTER(i)]
     L.probe_head_bytes.restype = l
@@ -79,10 +79,12 @@ def test_cuts_of_prompts_cover_every_query(probe):
     for _ in range(1000):
         n, heads, group, D = rng.choice([1, 3, 40]), rng.choice([1, 4, 16]), rng.choice([1, 5, 8]), rng.choice([64, 96, 128])
         tokens = int(2 ** rng.uniform(0, 16))
-        p = _plan(probe.probe_prompt_plan, n, heads, group, D, tokens)
+        window, sinks = rng.choice([(NONE, 0), (1, 0), (35, 4), (2048, 4)])
+        p = _plan(probe.probe_prompt_plan, n, heads, group, D, tokens, window, sinks)
         assert p["col_blocks"] * p["waves"] >= -(-tokens // 32) * group > (p["col_blocks"] - 1) * p["waves"]
         assert p["splits"] == 1 and p["workspace"] == 0 and p["groups"] == n * heads * p["col_blocks"]
         assert p["waves"] == 4 or (p["waves"] == 8 and D > 64 and p["groups"] >= 256)
+        assert p["waves"] == 4 or D == 128 or min(tokens, window + sinks) >= 1536
 
 
 def test_every_workgroup_has_a_place_of_its_own(probe):
