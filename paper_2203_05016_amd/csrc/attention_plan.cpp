@@ -23,7 +23,12 @@ AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t to
 {
     AttnPlan p = {};
     const int64_t pairs = (int64_t)batch * heads, columns = (int64_t)group * max_queries;
-    p.decode = columns <= 64;
+    // The kernel for few queries up to 64 columns (8 sequences of 4000 keys, 8 queries of 64 heads over 8 of 128: 27 us, in tiles of queries 42;
+    // 24 of up to 3001, 5 queries: 34 and 100), and up to 128 in blocks of 32, each of which reads the cache, while the GPU holds them: 16
+    // queries of the same heads over 3000 keys, 16 sequences 47 us and 60, 64 of them over 1000 keys 103 and 74.
+    const bool cuts = group <= 32;                 // blocks are of whole queries
+    const int64_t blocks_of_32 = cuts ? ceil_div(max_queries, 32 / group) : 1;
+    p.decode = columns <= 64 || (cuts && columns <= 128 && pairs * blocks_of_32 <= 2 * CUS);
     int64_t slots, least;   // workgroups the GPU holds at a time, and tiles that a part is worth
     if (p.decode) {
         p.col_tiles = (int)ceil_div(columns, 16);
@@ -31,9 +36,9 @@ AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t to
         // 64 columns leave one wavefront per SIMD (D = 128): two blocks of 32, of whole queries, read the cache twice and are faster.  16
         // sequences of 3000 keys on average, 8 queries of 64 heads over 8 of 128: 48 -> 35 us; 32 of them 66 -> 54; of 64 features
         // 28 -> 24; but 24 of 2100, 5 queries, in 48 columns 34 and in two blocks 41.
-        if (p.col_tiles == 4 && group <= 32) {
+        if (p.col_tiles >= 4 && cuts) {
             p.col_tiles = 2;
-            p.col_blocks = (int)ceil_div(max_queries, 32 / group);
+            p.col_blocks = (int)blocks_of_32;
         }
         // Workgroups of 8 wavefronts while all of them are on the GPU at a time, of 4 beyond: 64 sequences of 2500 keys on average, 8 heads
         // of 128: 40 us with 8, 44 with 4; 128 of 1028, 16 heads of 64: 35 and 29.
@@ -43,6 +48,8 @@ AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t to
         least = 4 * p.waves;
     } else {
         const int64_t items = ceil_div(max_queries, ATTN_TILE_QUERIES) * group;
+        // 8 wavefronts share what they bring; 4 where there are no more items (4 sequences of up to 9000 keys, 1024 queries, 32 heads over 8 of
+        // 96 410 us with 8, 428 with 4)
         p.waves = items > 4 ? 8 : 4;
         p.col_blocks = (int)ceil_div(items, p.waves);
         slots = p.waves == 4 && D < 128 ? 2 * CUS : CUS;   // what the LDS holds of three tiles

@@ -115,6 +115,18 @@ def test_many_tokens_each(dtype, D, heads, group, page):
     for window, sinks in MASKS:
         announce("chunk", dtype, D, heads, group, page, window, sinks)
         got = s.run(q, counts, window=window, sinks=sinks)
+        assert ("decode_kernel<%d,32 columns" if group == 1 else "tile_kernel<%d,cache") % D in binding.last_kernel()
+        check(got, *s.want(q, counts, window=window, sinks=sinks), "window %d sinks %d" % (window, sinks))
+
+
+@pytest.mark.parametrize("D", [64, 96, 128])
+def test_more_tokens_of_single_heads(D):
+    lengths, counts = [200, 3, 300], [140, 3, 129]
+    s = Served(lengths, 2, D, 32, torch.float16, seed=23)
+    q = _tensor(2 * D, sum(counts), torch.float16, 54)
+    for window, sinks in MASKS:
+        announce("more tokens", D, window, sinks)
+        got = s.run(q, counts, window=window, sinks=sinks)
         assert "tile_kernel<%d,cache" % D in binding.last_kernel()
         check(got, *s.want(q, counts, window=window, sinks=sinks), "window %d sinks %d" % (window, sinks))
 
