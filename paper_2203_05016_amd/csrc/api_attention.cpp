@@ -127,7 +127,7 @@ int shflbw_window_attention(const void* q, int64_t ldq, const void* k, int64_t l
     if (!q || !k || !v || !out) return fail(SHFLBW_ERR_NULL_ARG, "q, k, v and out must not be NULL");
     if (ldq < tokens || ldk < tokens || ldv < tokens || ldo < tokens) return fail(SHFLBW_ERR_BAD_SHAPE, "leading dimension too small");
     if (ldk >= ATTN_MAX_LD || ldv >= ATTN_MAX_LD) return fail(SHFLBW_ERR_BAD_SHAPE, "leading dimensions of k and v must be below 2^26");
-    const AttnPlan plan = plan_prompt(sequences, heads, q_heads / heads, head_dim, max_tokens, window ? window : INT_MAX, sinks);
+    const AttnPlan plan = plan_prompt(sequences, heads, q_heads / heads, head_dim, max_tokens, window ? window : INT_MAX, sinks, tokens);
     AttnArgs a = {};
     a.q = static_cast<const uint16_t*>(q);
     a.k = static_cast<const uint16_t*>(k);

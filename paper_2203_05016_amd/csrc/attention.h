@@ -75,6 +75,7 @@ struct AttnPlan {
     bool decode;              // the kernel for few queries
     int col_tiles;            // its 16-column tiles per wavefront
     int waves;                // wavefronts per workgroup
+    bool tiny;                // the other's form for a prompt of fewer than 64 columns in all
     int col_blocks, splits, split_tiles;
     int64_t groups;           // workgroups
     int64_t workspace;        // bytes
@@ -99,8 +100,13 @@ SHFLBW_HD inline AttnPlace attn_place(int block, int pairs, int heads, int per_p
 
 // How attention over the cache is cut.  max_queries, max_length: of any sequence.
 AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t tokens, int max_queries, int64_t max_length, int window, int sinks);
-// The same for prompts, which need no workspace
-AttnPlan plan_prompt(int sequences, int heads, int group, int D, int64_t max_tokens, int window, int sinks);
+// The same for prompts, which need no workspace.  tokens: columns in all.
+AttnPlan plan_prompt(int sequences, int heads, int group, int D, int64_t max_tokens, int window, int sinks, int64_t tokens = ATTN_TILE_KEYS);
+// Which forms of the tile kernel there are: the launcher has these and no others, and a plan names one of them
+constexpr bool tile_kernel_exists(int D, bool cache, int waves, bool tiny)
+{
+    return tiny ? !cache && waves == 4 : waves == 4 || (waves == 8 && (cache || D > 64));
+}
 
 // SHFLBW_OK, or why the cache cannot be used (host checks of its fields)
 int check_cache(const shflbw_kv_cache* cache);

@@ -71,15 +71,17 @@ AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t to
     return p;
 }
 
-AttnPlan plan_prompt(int sequences, int heads, int group, int D, int64_t max_tokens, int window, int sinks)
+AttnPlan plan_prompt(int sequences, int heads, int group, int D, int64_t max_tokens, int window, int sinks, int64_t tokens)
 {
     AttnPlan p = {};
+    p.tiny = tokens < ATTN_TILE_KEYS;    // whole tiles of keys would reach past the rows
     const int64_t items = ceil_div(max_tokens, ATTN_TILE_QUERIES) * group, pairs = (int64_t)sequences * heads;
     // Workgroups of 8 wavefronts share what they bring to the LDS; of 4 where 8 leave CUs without work, for heads of 64 (tile_residency), and
     // for heads of 96, of which a CU holds two, where their keys are few: 8 prompts of 4096, 8 heads, windows of 64, 512 and 1024 61, 99 and 147 us
     // in these, 70, 114 and 152 in workgroups of 8; without a window, 4 of up to 4096, 32 over 8 heads, 487 and 452.
     const bool few_keys = keys_seen(max_tokens, window, sinks, 0) < 1536;
-    p.waves = D > 64 && !(D == 96 && few_keys) && ceil_div(items, 8) * pairs >= CUS ? 8 : 4;
+    // Fewer than 64 columns: in workgroups of 4.
+    p.waves = !p.tiny && D > 64 && !(D == 96 && few_keys) && ceil_div(items, 8) * pairs >= CUS ? 8 : 4;
     p.col_blocks = (int)ceil_div(items, p.waves);
     p.splits = 1;
     p.split_tiles = INT32_MAX;

@@ -1,0 +1,43 @@
+"""The attention operators at the limits of what a call may ask for.  No GPU."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+from paper_2203_05016_amd import build as lib_build
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+NONE = 2 ** 31 - 1       # no window
+
+
+@pytest.fixture(scope="module")
+def probe(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("limits") / "attention_limits_probe.so")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", lib_build.CSRC,
+                           "-I", os.path.join(os.path.dirname(HERE), "include"), os.path.join(HERE, "attention_limits_probe.cpp"),
+                           os.path.join(lib_build.CSRC, "attention_plan.cpp"), "-o", so])
+    L = ctypes.CDLL(so)
+    i, l = ctypes.c_int, ctypes.c_long
+    L.probe_prompt_kernel.argtypes = [i, i, i, i, l, i, i, l, ctypes.POINTER(i)]
+    return L
+
+
+def test_the_kernel_that_is_launched_covers_every_query_of_a_prompt(probe):
+    """All column counts around one tile of keys, many sequences and heads: the kernel named exists, is the form for fewer than 64
+    columns exactly there, and its workgroups have an item for every block of queries of every head."""
+    out = (ctypes.c_int * 3)()
+    named = set()
+    for tokens in list(range(1, 67)) + [100, 5000]:
+        for sequences in (1, 2, 16, 20, 32, 64, 300):
+            for heads in (1, 4, 8, 16, 32):
+                for group in (1, 5, 8, 16):
+                    for D in (64, 96, 128):
+                        for most in {1, -(-tokens // sequences), tokens}:
+                            for window, sinks in ((NONE, 0), (16, 2)):
+                                assert probe.probe_prompt_kernel(sequences, heads, group, D, most, window, sinks, tokens, out)
+                                waves, tiny, blocks = out
+                                assert tiny == (tokens < 64) and (waves == 4 or not tiny)
+                                assert blocks * waves >= -(-most // 32) * group, (tokens, sequences, heads, group, D, most)
+                                named.add((D, waves, tiny))
+    assert named == {(64, 4, 0), (96, 4, 0), (96, 8, 0), (128, 4, 0), (128, 8, 0), (64, 4, 1), (96, 4, 1), (128, 4, 1)}
