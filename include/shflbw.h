@@ -314,9 +314,10 @@ int shflbw_kv_read(const shflbw_kv_cache* cache, const int32_t* slots, int64_t t
  *  starts       device, batch + 1: sequence b's queries are columns starts[b] to
  *               starts[b + 1] - 1, in order.  NULL: one each, column b (tokens ==
  *               batch, max_queries == 1).  Columns of no sequence are left undefined.
- *  max_queries, max_length  at least what any sequence has: queries past the
- *               former are left undefined; the latter decides how the work is
- *               cut, never what is computed.
+ *  max_queries  at least what any sequence has: queries past it are left undefined.
+ *  max_length   the longest sequence's tokens, as far as the host knows them: decides how the
+ *               work is cut, never what is computed.  Sequences that are longer are
+ *               attended to whole (the call takes longer), as those of a captured call may grow to be.
  *  window       0: none
  * The struct is host memory; what it points to is device memory.
  */

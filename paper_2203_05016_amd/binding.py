@@ -524,8 +524,8 @@ class KVCache:
 
         q (q_heads * head_dim, tokens): sequence b's queries are columns ``starts[b]`` to ``starts[b + 1] - 1``; without
         starts every sequence has one, column b.  table (batch, pages) int32: the sequence's pages in order.
-        lengths (batch,) int32: its tokens in the cache.  max_queries and max_length: at least what any sequence has
-        (max_length: all of the table's pages by default).  window 0 is none; the first ``sinks`` tokens stay visible
+        lengths (batch,) int32: its tokens in the cache.  max_queries: at least what any sequence has.  max_length: of the longest
+        (all of the table's pages by default); it decides how the work is cut, and sequences past it only take longer.  window 0 is none; the first ``sinks`` tokens stay visible
         past it.  What is on the GPU is not looked at by the host: see shflbw_kv_sequences for what bad entries do."""
         if stream is None and self._plan is not None:
             r = _calls.kv_attention(self._plan, q, table, lengths, starts, max_queries, max_length, window, sinks, out)

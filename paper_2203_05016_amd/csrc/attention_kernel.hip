@@ -218,7 +218,8 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
     const int p_first = seq.len - left, p_last = p_first + (cols - 1) / a.group;
     const AttnTiles tiles = attn_tiles(p_first, p_last, a.window, a.sinks, 0, ATTN_DECODE_KEYS);
     const int v_begin = split * a.split_tiles;
-    const int v_end = tiles.count - v_begin < a.split_tiles ? tiles.count : v_begin + a.split_tiles;
+    // the last part takes what is left, also of a sequence longer than the plan was told
+    const int v_end = split + 1 == a.splits || tiles.count - v_begin < a.split_tiles ? tiles.count : v_begin + a.split_tiles;
 
     const int page = 1 << a.page_shift;
     const int64_t chunk = page_head_bytes(page, D), page_bytes = chunk * a.heads;
@@ -560,7 +561,7 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
     const int wg_last = position(item_last / a.group * ATTN_TILE_QUERIES + ATTN_TILE_QUERIES - 1);
     const AttnTiles tiles = attn_tiles(wg_first, wg_last, a.window, a.sinks, shift, ATTN_TILE_KEYS);
     const int v_begin = split * (a.splits > 1 ? a.split_tiles : 0);
-    const int v_end = a.splits == 1 || tiles.count - v_begin < a.split_tiles ? tiles.count : v_begin + a.split_tiles;
+    const int v_end = split + 1 == a.splits || tiles.count - v_begin < a.split_tiles ? tiles.count : v_begin + a.split_tiles;   // (as in the other kernel)
 
     // the wavefront's item; one that is not there repeats the last one, needs no keys, and its result is dropped
     const bool works = item0 + wave <= item_last;

@@ -6,7 +6,7 @@ import torch
 from attention_reference import attend, check
 from gpu_util import announce
 from paper_2203_05016_amd import binding
-from test_attention_gpu import DEV, NAN, _tensor
+from test_attention_gpu import DEV, NAN, Served, _tensor
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +31,18 @@ def test_short_prompts_of_many_sequences(D, heads, group, counts):
             part = [x[:, at:at + n].double().numpy() for x in (q, k, v)]
             check(out[:, at:at + n], *attend(*part, D, 0, torch.bfloat16), "columns %d to %d" % (at, at + n - 1))
         at += n
+
+
+@pytest.mark.parametrize("counts,max_length,parts", [(None, 64, False), (None, 1, False), (None, 2100, True), ([5, 3], 100, False), ([5, 3], 2100, True),
+                                                     ([80, 41], 100, False), ([80, 41], 1000, True)])
+@pytest.mark.parametrize("D,group", [(64, 4), (128, 8)])
+def test_lengths_past_max_length(D, group, counts, max_length, parts):
+    """max_length decides how the work is cut, never what is computed: sequences that have grown past it see all their keys."""
+    announce("past max_length", D, group, counts, max_length)
+    s = Served([3500, 2777], 1, D, 64, torch.float16, seed=14)
+    q = _tensor(group * D, sum(counts) if counts else 2, torch.float16, 66)
+    seqs = binding._Sequences(group, 2, max(counts or [1]), s.table.shape[1], 0, 0, q.shape[1], max_length, s.table.shape[1], None, None, 1 if counts else None)
+    assert (binding.lib().shflbw_kv_attention_workspace(s.cache._c, seqs) > 0) == parts
+    for window, sinks in [(0, 0), (2200, 70)]:
+        got = s.run(q, counts, window=window, sinks=sinks, max_length=max_length)
+        check(got, *s.want(q, counts or [1, 1], window=window, sinks=sinks), "window %d" % window)
