@@ -20,6 +20,8 @@ def probe(tmp_path_factory):
     L = ctypes.CDLL(so)
     i, l = ctypes.c_int, ctypes.c_long
     L.probe_prompt_kernel.argtypes = [i, i, i, i, l, i, i, l, ctypes.POINTER(i)]
+    L.probe_cache_blocks.argtypes = [i, i, i, i, l, i, l, ctypes.POINTER(l)]
+    L.probe_cache_blocks.restype = None
     return L
 
 
@@ -41,3 +43,24 @@ def test_the_kernel_that_is_launched_covers_every_query_of_a_prompt(probe):
                                 assert blocks * waves >= -(-most // 32) * group, (tokens, sequences, heads, group, D, most)
                                 named.add((D, waves, tiny))
     assert named == {(64, 4, 0), (96, 4, 0), (96, 8, 0), (128, 4, 0), (128, 8, 0), (64, 4, 1), (96, 4, 1), (128, 4, 1)}
+
+
+def test_a_generous_bound_of_queries_cuts_as_the_columns_do(probe):
+    """No sequence has more queries than there are columns in all."""
+    one, two = (ctypes.c_long * 3)(), (ctypes.c_long * 3)()
+    for batch in (1, 3, 64):
+        for group in (1, 8, 33, 65535):
+            for D in (64, 128):
+                for tokens in (1, 7, 64, 1000):
+                    probe.probe_cache_blocks(batch, 2, group, D, tokens, tokens, 5000, one)
+                    for most in (tokens + 1, 100000, 2 ** 31 - 1):
+                        probe.probe_cache_blocks(batch, 2, group, D, tokens, most, 5000, two)
+                        assert list(one) == list(two) and one[0] > 0 and one[1] > 0, (batch, group, D, tokens, most, list(two))
+
+
+def test_more_workgroups_than_a_launch_takes_are_counted_as_such(probe):
+    """Never as few, or fewer than none: the launcher refuses by this number."""
+    out = (ctypes.c_long * 3)()
+    for batch, heads, group, tokens in ((1, 1, 65535, 2 ** 31 - 1), (2 ** 31 - 1, 16384, 3, 2 ** 31 - 1), (1000, 16384, 4, 2 ** 31 - 1)):
+        probe.probe_cache_blocks(batch, heads, group, 128, tokens, 2 ** 31 - 1, 5000, out)
+        assert out[1] > 2 ** 31 - 1 and out[0] > 0, list(out)

@@ -46,3 +46,16 @@ def test_lengths_past_max_length(D, group, counts, max_length, parts):
     for window, sinks in [(0, 0), (2200, 70)]:
         got = s.run(q, counts, window=window, sinks=sinks, max_length=max_length)
         check(got, *s.want(q, counts or [1, 1], window=window, sinks=sinks), "window %d" % window)
+
+
+@pytest.mark.parametrize("counts", [[5, 3], [80, 41]])
+def test_a_generous_bound_of_queries(counts):
+    announce("generous max_queries", counts)
+    D, group = 64, 4
+    s = Served([250, 177], 1, D, 64, torch.bfloat16, seed=16)
+    q = _tensor(group * D, sum(counts), torch.bfloat16, 68).to(DEV)
+    table, lengths = s.table.to(DEV), torch.tensor(s.lengths, dtype=torch.int32, device=DEV)
+    want = s.cache.attention(q, table, lengths, _starts(counts), max_queries=sum(counts))
+    check(want, *s.want(q.cpu(), counts))
+    for most in (1000, 2 ** 31 - 1):
+        assert torch.equal(want, s.cache.attention(q, table, lengths, _starts(counts), max_queries=most))
