@@ -7,7 +7,6 @@ stream handle; numpy arrays for host-side inputs of the compressor.
 The library is required: if ``libshflbw.so`` has not been built this module
 raises at first use.  There is no CPU fallback.
 """
-import contextlib
 import ctypes
 import os
 
@@ -179,6 +178,24 @@ def _stream_ptr(stream):
     return s.cuda_stream
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory of the stream that the work runs on: what was there before it, and what comes after, is ordered with it."""
+    import torch
+    if stream is None or torch.device(device).type != "cuda":
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _result(shape, dtype, device, stream):
+    """The same for what the caller gets, whose own (current) stream may still read it when it is let go."""
+    import torch
+    t = _empty(shape, dtype, device, stream)
+    if stream is not None and t.is_cuda:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
 _YDTYPE = None   # torch dtype -> shflbw_dtype, filled on first use (torch is imported lazily)
 
 
@@ -262,7 +279,7 @@ class Matrix:
     # -- device side
     def bind_device(self, device="cuda:0", stream=None):
         import torch
-        buf = torch.empty(self.device_bytes(), dtype=torch.uint8, device=device)
+        buf = _result(self.device_bytes(), torch.uint8, device, stream)
         _check(lib().shflbw_bind_device(self._h, ctypes.c_void_p(buf.data_ptr()),
                                         _stream_ptr(stream)))
         self._dev = buf
@@ -308,9 +325,7 @@ class Matrix:
             _ydtype(Y)
         self._require_on_bound_device(X, "X")
         if Y is None:
-            import torch
-            Y = torch.empty((info["M"], N), dtype=out_dtype or self._operand_dtype(),
-                            device=X.device)
+            Y = _result((info["M"], N), out_dtype or self._operand_dtype(), X.device, stream)
         else:
             self._require_on_bound_device(Y, "Y")
         ldx = X.stride(0) if K > 1 else max(N, 1)
@@ -330,7 +345,6 @@ class Matrix:
                 if rc < 0:
                     _check(rc)
                 return out
-        import torch
         if inp.dtype != self._operand_dtype() or not inp.is_contiguous() or inp.dim() != 4:
             raise TypeError("input must be a contiguous 4-D %s tensor" % self._operand_dtype())
         if layout not in ("NCHW", "CHWN"):
@@ -354,7 +368,7 @@ class Matrix:
             _ydtype(out)
         self._require_on_bound_device(inp, "input")
         if out is None:
-            out = torch.empty(shape, dtype=out_dtype or self._operand_dtype(), device=inp.device)
+            out = _result(shape, out_dtype or self._operand_dtype(), inp.device, stream)
         else:
             self._require_on_bound_device(out, "out")
         _check(lib().shflbw_conv2d(self._h, inp.data_ptr(), out.data_ptr(), B, C, H, W, R, S,
@@ -404,13 +418,13 @@ def layernorm_transpose(x, gamma=None, beta=None, eps=1e-5, normalize=True, out=
     for t in (gamma, beta):
         if t is not None and (t.dtype != x.dtype or t.shape != (K,) or not t.is_contiguous()):
             raise TypeError("gamma and beta must be contiguous (K,) tensors of x's dtype")
-    if out is None:
-        out = torch.empty((K, N), dtype=x.dtype, device=x.device)
-    if out.dtype != x.dtype or out.shape != (K, N) or out.stride(1) != 1:
+    if out is not None and (out.dtype != x.dtype or out.shape != (K, N) or out.stride(1) != 1):
         raise TypeError("out must be a (K, N) tensor of x's dtype with unit token stride")
     for t in (x, out, gamma, beta):
         if t is not None and (not t.is_cuda or t.device != x.device):
             raise ValueError("x, gamma, beta and out must live on one GPU")
+    if out is None:
+        out = _result((K, N), x.dtype, x.device, stream)
     if (N > 1 and x.stride(0) < K) or (K > 1 and out.stride(0) < N):
         raise ValueError("rows of x or out overlap")
     ptr = lambda t: ctypes.c_void_p(None if t is None else t.data_ptr())
@@ -510,11 +524,10 @@ class KVCache:
                 if type(both) is int:
                     _check(both)
                 return both
-        import torch
         n, rows = slots.shape[0] if slots.dim() else 0, self.heads * self.head_dim
         _indices(slots, "slots", n)
         _on(self.device, slots=slots, k=k, v=v)
-        k, v = (torch.empty((rows, n), dtype=self.dtype, device=self.device) if t is None else t for t in (k, v))
+        k, v = (_result((rows, n), self.dtype, self.device, stream) if t is None else t for t in (k, v))
         ldk, ldv = _columns(k, "k", rows, self.dtype, n), _columns(v, "v", rows, self.dtype, n)
         _check(lib().shflbw_kv_read(self._c, slots.data_ptr(), n, k.data_ptr(), ldk, v.data_ptr(), ldv, _stream_ptr(stream)))
         return k, v
@@ -552,17 +565,13 @@ class KVCache:
         _natural(max_queries=max_queries, max_length=max_length, window=window, sinks=sinks)
         _on(self.device, q=q, table=table, lengths=lengths, starts=starts, out=out)
         if out is None:
-            out = torch.empty((rows, tokens), dtype=self.dtype, device=self.device)
+            out = _result((rows, tokens), self.dtype, self.device, stream)
         ldo = _columns(out, "out", rows, self.dtype, tokens)
         s = _Sequences(rows // self.head_dim, batch, max_queries, width, window, sinks, tokens, max_length,
                        table.stride(0) if batch > 1 else width, table.data_ptr(), lengths.data_ptr(),
                        None if starts is None else starts.data_ptr())
         size = _check(lib().shflbw_kv_attention_workspace(self._c, s))
-        work = None
-        if size:
-            # memory of the stream that the work runs on: what was there before it, and what comes after, is ordered with it
-            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
-                work = torch.empty(size, dtype=torch.uint8, device=self.device)
+        work = _empty(size, torch.uint8, self.device, stream) if size else None
         _check(lib().shflbw_kv_attention(self._c, s, q.data_ptr(), ldq, out.data_ptr(), ldo, work.data_ptr() if size else None, size,
                                          _stream_ptr(stream)))
         return out
@@ -597,7 +606,7 @@ def window_attention(q, k, v, head_dim, starts=None, max_tokens=None, window=0, 
     _natural(max_tokens=max_tokens)
     _on(q.device, q=q, k=k, v=v, starts=starts, out=out)
     if out is None:
-        out = torch.empty((rows, tokens), dtype=q.dtype, device=q.device)
+        out = _result((rows, tokens), q.dtype, q.device, stream)
     ldo = _columns(out, "out", rows, q.dtype, tokens)
     _check(lib().shflbw_window_attention(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, out.data_ptr(), ldo,
                                          rows // head_dim, k.shape[0] // head_dim, head_dim, tokens,
