@@ -271,7 +271,9 @@ int shflbw_layernorm_transpose(const void* x, int64_t ldx, const void* gamma, co
  * infinity or a NaN is stored as NaN as a whole.
  *
  *  data         device, caller-owned, shflbw_kv_cache_bytes bytes, 128-byte
- *               aligned.  Slots that were never written hold what was there.
+ *               aligned.  Slots that were never written hold what was there: whatever
+ *               that is, it never reaches a query that does not see them; to one that does
+ *               its values mean nothing.
  *  pages, page_tokens  page_tokens is a power of two from 32 to 1024, pages *
  *               page_tokens below 2^31.  Slot = page * page_tokens + place in
  *               the page.

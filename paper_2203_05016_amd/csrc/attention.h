@@ -25,6 +25,9 @@
 
 namespace shflbw {
 
+// The largest scale byte of a finite block: of 65504 (binary16), of exponent 127 (bfloat16).  Larger ones are in slots that were never written, or 255:
+// 16 bits may not hold their values, so attention keeps them from queries that do not see them as it does NaN.
+SHFLBW_HD constexpr unsigned most_scale(bool bf16) { return bf16 ? 252 : 140; }
 SHFLBW_HD constexpr int scale_bytes(int D) { return D == 64 ? 2 : 4; }   // a token's scales, as one load
 SHFLBW_HD constexpr int64_t page_head_bytes(int page, int D) { return (int64_t)page * (D + 2 * scale_bytes(D)); }
 // Which 16-byte (12 for D = 96; 8 of 16 for D = 64) piece of its 16 tokens a token's words of q (0..3) are

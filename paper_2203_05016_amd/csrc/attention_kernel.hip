@@ -334,7 +334,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int s = 0; s < S; ++s)
-                    if ((raw.vs[u] >> 8 * s & 255) == 255) {
+                    if ((raw.vs[u] >> 8 * s & 255) > most_scale(BF)) {
                         special = true;
                         raw.vs[u] &= ~(255u << 8 * s);
                         raw.v[u][s] = 0;
@@ -422,7 +422,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
                     if (attn_sees(j, p[n], lo[n], a.sinks))
 #pragma unroll
                         for (int t = 0; t < DT; ++t)
-                            if (!there || (unsigned char)scales[t / 2] == 255) o[n][t] += __builtin_nanf("");
+                            if (!there || (unsigned char)scales[t / 2] > most_scale(BF)) o[n][t] += __builtin_nanf("");
             }
         }
 
@@ -689,7 +689,7 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
         if constexpr (CACHE) {
 #pragma unroll
             for (int s = 0; s < UNITS; ++s)
-                if ((codes[n] >> 8 * s & 255) == 255) {
+                if ((codes[n] >> 8 * s & 255) > most_scale(BF)) {
                     found = true;
                     codes[n] &= ~(255u << 8 * s);
                     word[n][s] = 0;
@@ -898,7 +898,7 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
                     const char* sc8 = pages + (there ? id : 0) * page_bytes + (int64_t)page * D + (int64_t)(page + (k & (page - 1))) * SB;
 #pragma unroll
                     for (int t = 0; t < DT; ++t)
-                        if (!there || (unsigned char)sc8[t] == 255) o[t] += __builtin_nanf("");
+                        if (!there || (unsigned char)sc8[t] > most_scale(BF)) o[t] += __builtin_nanf("");
                 } else {
 #pragma unroll
                     for (int t = 0; t < DT; ++t)

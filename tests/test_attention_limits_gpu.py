@@ -59,3 +59,19 @@ def test_a_generous_bound_of_queries(counts):
     check(want, *s.want(q.cpu(), counts))
     for most in (1000, 2 ** 31 - 1):
         assert torch.equal(want, s.cache.attention(q, table, lengths, _starts(counts), max_queries=most))
+
+
+@pytest.mark.parametrize("counts", [None, [5, 3], [80, 41]])
+@pytest.mark.parametrize("dtype,byte", [(torch.float16, 200), (torch.float16, 254), (torch.bfloat16, 254)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_slots_that_were_never_written(D, dtype, byte, counts):
+    """They hold what was there: here codes and scales whose values 16 bits cannot hold, which no query sees."""
+    announce("never written", D, dtype, byte, counts)
+    s = Served([250, 177], 2, D, 32, dtype, seed=15)
+    s.cache._dev.fill_(byte)
+    for b, n in enumerate(s.lengths):
+        s.put(b, _tensor(2 * D, n, dtype, 400 + b), _tensor(2 * D, n, dtype, 500 + b, 0))
+    q = _tensor(4 * D, sum(counts) if counts else 2, dtype, 67)
+    for window, sinks in [(0, 0), (70, 5)]:
+        got = s.run(q, counts, window=window, sinks=sinks)
+        check(got, *s.want(q, counts or [1, 1], window=window, sinks=sinks), "window %d" % window)
