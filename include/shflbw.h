@@ -342,7 +342,8 @@ int64_t shflbw_kv_attention_workspace(const shflbw_kv_cache* cache, const shflbw
  *          contents are free again when the call's work has ended.  NULL where 0 bytes are needed.
  * Scores, softmax and sums are in binary32, weights are rounded to dtype for
  * their product with the values.  Keys and values that a query does not see
- * never reach its result, whatever they hold.  Two calls with the same
+ * never reach its result, whatever they hold; infinities and NaN among the values that it
+ * sees are its result's as their sum, however small their weights.  Two calls with the same
  * arguments give the same bits.  Enqueues on `stream` only.
  */
 int shflbw_kv_attention(const shflbw_kv_cache* cache, const shflbw_kv_sequences* sequences, const void* q, int64_t ldq,

@@ -493,7 +493,9 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
 // by issue: matrix units are busy in 52, 44 and 30 % of the cycles, vector instructions issued in 53, 48 and 65 %, the clock falls to 1.9 GHz.
 //
 // Infinities and NaN among the values of a tile that not all of the workgroup's queries see whole are zeros in the LDS, so that
-// they do not reach a query that does not see them as 0 * NaN; if there were any, they are added where they are seen at the end.
+// they do not reach a query that does not see them as 0 * NaN; if there were any, they are added where they are seen at the end.  In tiles that all
+// see whole an infinity becomes NaN where its weight was rounded to zero, or the sum scaled down by zero: sums of prompts that are not finite at the end are
+// worked out again (attn_infinite_sums).
 constexpr int ATTN_AHEAD = 2;              // an operand is read this many steps of the reduction before its product
 
 template <bool BF, int D, bool CACHE>
@@ -527,6 +529,52 @@ __device__ __forceinline__ void attn_hide(int from, int p, int lo, int least, in
 #pragma unroll
     for (int i = 0; i < N; ++i)
         if ((unsigned)(key(i) - offset) > span) hide(i);
+}
+
+// Sums of features whose values are not finite in the tiles that all of the workgroup's queries see whole: those values' sum in place of what their
+// products with weights came to.  A lane takes 8 of a tile's 64 keys in every eighth row; its bit i of a mask is row 8 i + lane / 8.
+template <bool BF, int D, class FirstKey, class Partial>
+__device__ __forceinline__ void attn_infinite_sums(float16v (&o)[D / 32], const uint16_t* values, int64_t ld, int v_begin, int v_end, FirstKey&& first_key, Partial&& partial)
+{
+    constexpr unsigned SIZE = 0x7fffu, INF = BF ? 0x7f80u : 0x7c00u;
+    const int lane = threadIdx.x & 63;
+    unsigned up = 0, down = 0, none = 0;                   // rows with +infinity, -infinity, NaN
+    for (int v = v_begin; v < v_end; ++v) {
+        const int j = first_key(v);
+        if (partial(j)) continue;
+        const uint16_t* src = values + (lane >> 3) * ld + j + (lane & 7) * 8;
+#pragma unroll 4
+        for (int i = 0; i < D / 8; ++i) {
+            uint4v x;
+            __builtin_memcpy(&x, src + i * 8 * ld, 16);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const unsigned one = x[k / 2] >> 16 * (k % 2) & 0xffffu, size = one & SIZE;
+                up |= (one == INF ? 1u : 0u) << i;
+                down |= (one == (INF | 0x8000u) ? 1u : 0u) << i;
+                none |= (size > INF ? 1u : 0u) << i;
+            }
+        }
+    }
+#pragma unroll
+    for (int by = 1; by < 8; by *= 2) {
+        up |= __shfl_xor(up, by);
+        down |= __shfl_xor(down, by);
+        none |= __shfl_xor(none, by);
+    }
+    // this lane's features are 32 t + 8 (e / 4) + 4 (lane / 32) + e % 4
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int from = 8 * (4 * (lane >> 5) + r);
+        const unsigned row_up = __shfl(up, from), row_down = __shfl(down, from), row_none = __shfl(none, from);
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            const int e = 4 * (i % 4) + r;
+            if (row_up >> i & 1) o[i / 4][e] = INFINITY;
+            if (row_down >> i & 1) o[i / 4][e] = -INFINITY;
+            if ((row_none | (row_up & row_down)) >> i & 1) o[i / 4][e] = __builtin_nanf("");
+        }
+    }
 }
 
 // TINY: a prompt of fewer than 64 columns in all.
@@ -886,6 +934,15 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
 #pragma unroll
             for (int t = 0; t < DT; ++t) o[t] = attn_mma32<BF>(value_operand(before, 2 + g, t), w[1][g], o[t]);
 
+    if constexpr (!CACHE && !TINY) {
+        float most = 0;                                    // infinity or NaN where a sum is not finite
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; e += 2)
+                most = __builtin_elementwise_maximum(__builtin_elementwise_maximum(__builtin_fabsf(o[t][e]), __builtin_fabsf(o[t][e + 1])), most);
+        if (__any(!(most < INFINITY) && l < INFINITY)) attn_infinite_sums<BF, D>(o, a.v + (int64_t)h * D * a.ldv + seq.t0, a.ldv, v_begin, v_end, first_key, partial);
+    }
     if (special)
         for (int v = v_begin; v < v_end; ++v) {
             const int from_key = first_key(v);

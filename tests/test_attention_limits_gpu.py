@@ -6,7 +6,7 @@ import torch
 from attention_reference import attend, check
 from gpu_util import announce
 from paper_2203_05016_amd import binding
-from test_attention_gpu import DEV, NAN, Served, _tensor
+from test_attention_gpu import DEV, INF, NAN, Served, _tensor
 
 pytestmark = pytest.mark.gpu
 
@@ -75,3 +75,31 @@ def test_slots_that_were_never_written(D, dtype, byte, counts):
     for window, sinks in [(0, 0), (70, 5)]:
         got = s.run(q, counts, window=window, sinks=sinks)
         check(got, *s.want(q, counts or [1, 1], window=window, sinks=sinks), "window %d" % window)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("D,group", [(64, 2), (96, 2), (128, 8)])
+@pytest.mark.parametrize("steep", [1, 10])
+def test_infinite_values_of_next_to_no_weight(dtype, D, group, steep):
+    """An infinity among the values a query sees is its result's, however small its weight and wherever its key lies: weights that
+    16 or 32 bits hold as zero, before the maximum (that the accumulators are scaled down for) and after it."""
+    n, step = 420, 14.0 if dtype == torch.float16 else 12.0
+    q, k, v = torch.full((group * D, n), steep * step / D ** 0.5, dtype=dtype), torch.zeros(D, n, dtype=dtype), _tensor(D, n, dtype, 33, 0)
+    top, deep = 200, 300                                  # scores: 0, at `top` that much more, at `deep` that much less
+    k[:, top], k[:, deep] = 8 / D ** 0.5, -8 / D ** 0.5
+    v[3, 10], v[17, deep], v[40, 10], v[40, deep], v[50, 350], v[60, 5] = INF, -INF, INF, -INF, NAN, -INF
+    clean = torch.where(torch.isfinite(v), v, 0)
+    for window, sinks in [(0, 0), (260, 0), (130, 8)]:
+        announce("infinite values", dtype, D, group, steep, window, sinks)
+        got = binding.window_attention(q.to(DEV), k.to(DEV), v.to(DEV), D, window=window, sinks=sinks)
+        want, tol = attend(*[x.double().numpy() for x in (q, k, clean)], D, 0, dtype, window=window, sinks=sinks)
+        p, j = np.arange(n)[:, None], np.arange(n)[None]
+        seen = (j <= p) & ((j > p - window) | (j < sinks) if window else True)
+        for f in (3, 17, 40, 50, 60):
+            special = np.where(torch.isfinite(v[f]).numpy(), 0, v[f].double().numpy())
+            with np.errstate(invalid="ignore"):
+                total = np.array([special[s].sum() for s in seen])
+            for h in range(group):
+                row = want[h * D + f]
+                row[total != 0] = total[total != 0]
+        check(got, want, tol, "window %d sinks %d" % (window, sinks))
