@@ -341,7 +341,8 @@ int64_t shflbw_kv_attention_workspace(const shflbw_kv_cache* cache, const shflbw
  *  workspace  device, 16-byte aligned, at least shflbw_kv_attention_workspace bytes; its
  *          contents are free again when the call's work has ended.  NULL where 0 bytes are needed.
  * Scores, softmax and sums are in binary32, weights are rounded to dtype for
- * their product with the values.  Keys and values that a query does not see
+ * their product with the values.  Scores beyond 2^24 in magnitude, whose steps in
+ * binary32 are no longer small beside 1, may give NaN.  Keys and values that a query does not see
  * never reach its result, whatever they hold; infinities and NaN among the values that it
  * sees are its result's as their sum, however small their weights.  Two calls with the same
  * arguments give the same bits.  Enqueues on `stream` only.

@@ -8,7 +8,8 @@
 // takes any order, as long as both operands have the same.
 //
 // Sums, maxima and accumulators are in 32 bits.  The weights are rounded to the operands' 16 bits for the second
-// product (relative 2^-12 or 2^-9 of each, beside the same rounding of the result).  Keys read from the cache are
+// product, which has no wider operands at its rate (half a step: relative 2^-11 or 2^-8 of each, beside the same rounding of the result; in binary16 at
+// most 2^-31 of the largest where they are subnormal).  Keys read from the cache are
 // exact in 16 bits but for binary16 blocks below 2^-21, whose values are rounded to multiples of 2^-24.
 //
 // A query whose mask leaves nothing gets zeros.  Infinities and NaN in keys or values that a query does not see leave
@@ -173,6 +174,11 @@ __device__ __forceinline__ int attn_window_start(int p, int window) { return p <
 // The maximum that scores are taken off follows the true one only when that has grown by this many powers of two: rescaling the
 // accumulators is rare then, and weights stay below 2^ATTN_SLACK.
 constexpr float ATTN_SLACK = 8;
+// In binary16 that maximum is taken 2^6 lower, so that all weights are 2^6 times as large: there are none below 2^-24, and a key of weight 1 beside
+// 40000 of 2^-26 lost all of these.  Now what is lost of a weight is at most 2^-31 of the largest.  The largest may be 2^(6 + ATTN_SLACK), a fourth of
+// what binary16 holds: room for the rounding of the maximum itself (half a step of it is below 2 while scores times log2(e) stay below 2^25).
+template <bool BF>
+constexpr float ATTN_LIFT = BF ? 0 : 6;
 // (not in assembly: matrix results need wait states before a vector instruction reads them, which the compiler puts in)
 __device__ __forceinline__ float attn_max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
@@ -369,14 +375,14 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
         for (int n = 0; n < NT; ++n) {
             const float4v x = sc[n][0], y = sc[n][1];
             top[n] = attn_max3(attn_max3(x[0], x[1], x[2]), attn_max3(x[3], y[0], y[1]), attn_max3(y[2], y[3], y[3])) * a.scale;
-            grown |= top[n] > m[n] + ATTN_SLACK;
+            grown |= top[n] > m[n] + (ATTN_SLACK + ATTN_LIFT<BF>);
         }
         if (__any(grown))
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 float2v t = attn_pair16(top[n]);
                 t = attn_pair32(attn_max3(t[0], t[1], t[1]));
-                const float now = attn_max3(t[0], t[1], m[n]), shrink = attn_exp2(m[n] - now);
+                const float now = fmaxf(fmaxf(t[0], t[1]) - ATTN_LIFT<BF>, m[n]), shrink = attn_exp2(m[n] - now);
                 m[n] = now;
                 l[n] *= shrink;
 #pragma unroll
@@ -840,8 +846,8 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
             } else if (u == 1) {
                 const float2v both = attn_pair32(top);
                 top = attn_max3(both[0], both[1], both[1]) * a.scale;
-                grown = top > m + ATTN_SLACK;
-                const float now = grown ? top : m;
+                grown = top > m + (ATTN_SLACK + ATTN_LIFT<BF>);
+                const float now = grown ? top - ATTN_LIFT<BF> : m;
                 shrink = attn_exp2(m - now);
                 m = now;
                 l *= shrink;

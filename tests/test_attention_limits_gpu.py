@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from attention_reference import attend, check
+from attention_reference import HALF_STEP, attend, check
 from gpu_util import announce
 from paper_2203_05016_amd import binding
 from test_attention_gpu import DEV, INF, NAN, Served, _tensor
@@ -103,3 +103,51 @@ def test_infinite_values_of_next_to_no_weight(dtype, D, group, steep):
                 row = want[h * D + f]
                 row[total != 0] = total[total != 0]
         check(got, want, tol, "window %d sinks %d" % (window, sinks))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_small_weights(D):
+    """One key of much weight and tens of thousands of 2^-26 of it: the sum of the weights and that of the weighted values leave none out.
+
+    Bound: a weight's rounding to binary16 is off by 2^-11 of it, or, of weights 2^6 times as large, by 2^-25 where they are subnormal: 2^-31
+    beside the largest; sums, exponentials and scores as in attention_reference."""
+    announce("small weights", D)
+    n, dtype = 40000, torch.float16
+    c = 26 * np.log(2.0)                                  # the first key's score beside the others' zeros
+    q = torch.full((D, n), c / D ** 0.5, dtype=dtype)
+    k, v = torch.zeros(D, n, dtype=dtype), torch.ones(D, n, dtype=dtype)
+    k[:, 0], v[:, 0] = 1, 0
+    got = binding.window_attention(q.to(DEV), k.to(DEV), v.to(DEV), D)
+    for p in (0, 1, 1000, 20000, 39999):
+        score = float(q[0, p].double()) * D ** 0.5
+        rest = p * np.exp(-score)
+        want = rest / (1 + rest)
+        tol = p * 2.0 ** -31 + want * (2 * HALF_STEP[dtype] + 2 * ((D + 4) * 2.0 ** -24 * score + 2.0 ** -22) + 2 * n * 2.0 ** -24) + 2.0 ** -25
+        off = (got[:, p].double() - want).abs().max().item()
+        assert off <= tol, (p, off, tol, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scores_up_to_sixteen_million(dtype, D):
+    """Scores whose steps in 32 bits are as large as 1, of both signs: which keys they pick is left open, but values that are the same for all
+    keys are what any weights give.  Bound: the weights' rounding (half a step above and below), the sum's of n of them, the result's."""
+    n, group = 300, 2
+    size = (1.5e7 / D ** 0.5) ** 0.5
+    g = torch.Generator().manual_seed(41)
+    rand = lambda rows: (size * (1 - torch.rand(rows, n, generator=g) / 64)).to(dtype)
+    q, k = rand(group * D), rand(D)
+    q[:, ::2] *= -1
+    v = (torch.rand(D, 1, generator=g) + 0.5).to(dtype).expand(D, n).contiguous()
+    assert 1e7 < float(q.double()[:D].abs().mul(k.double()).sum(0).max()) / D ** 0.5 < 1.6e7
+    announce("large scores", dtype, D)
+    tol = 3 * HALF_STEP[dtype] + 2 * n * 2.0 ** -24
+    got = binding.window_attention(q.to(DEV), k.to(DEV), v.to(DEV), D).double().cpu()
+    want = v.double().repeat(group, 1)
+    assert bool(((got - want).abs() <= tol * want).all()), ((got - want).abs() / want).max()
+    s = Served([n], 1, D, 32, dtype, seed=17)
+    s.put(0, k, v)
+    want = torch.from_numpy(s.v[0])[:, -1:].repeat(group, 1)
+    for nq in (1, 3, 90):
+        got = s.run(q[:, -nq:], [nq]).double().cpu()
+        assert bool(((got - want).abs() <= tol * want).all()), (nq, ((got - want).abs() / want).max())
