@@ -277,7 +277,8 @@ int shflbw_layernorm_transpose(const void* x, int64_t ldx, const void* gamma, co
  *  pages, page_tokens  page_tokens is a power of two from 32 to 1024, pages *
  *               page_tokens below 2^31.  Slot = page * page_tokens + place in
  *               the page.
- *  heads, head_dim  heads of keys (and of values); head_dim 64, 96 or 128.
+ *  heads, head_dim  heads of keys (and of values), up to 16384 (16383 of 128);
+ *               head_dim 64, 96 or 128.
  *  dtype        SHFLBW_F16 or SHFLBW_BF16: of everything that goes in or out.
  */
 typedef struct {
@@ -285,7 +286,8 @@ typedef struct {
     int32_t pages, page_tokens, heads, head_dim, dtype;
 } shflbw_kv_cache;
 
-/* Bytes of device memory of such a cache; 0 where the sizes are not supported. */
+/* Bytes of device memory of such a cache; 0 where the sizes are not supported
+ * (shflbw_last_error says why). */
 size_t shflbw_kv_cache_bytes(int pages, int page_tokens, int heads, int head_dim);
 
 /* Quantises column t of k and v (device, heads * head_dim x tokens, leading

@@ -483,9 +483,8 @@ class KVCache:
             raise TypeError("dtype must be float16 or bfloat16")
         _natural(pages=pages, page_tokens=page_tokens, heads=heads, head_dim=head_dim)
         size = int(lib().shflbw_kv_cache_bytes(pages, page_tokens, heads, head_dim))
-        if size == 0 or pages * page_tokens >= 2 ** 31:
-            raise ValueError("a cache has pages of a power of two from 32 to 1024 tokens, fewer than 2^31 slots and "
-                             "head_dim 64, 96 or 128 (got %d pages of %d, %d heads of %d)" % (pages, page_tokens, heads, head_dim))
+        if size == 0:
+            raise ValueError("%s (got %d pages of %d, %d heads of %d)" % (last_error(), pages, page_tokens, heads, head_dim))
         self.pages, self.page_tokens, self.heads, self.head_dim, self.dtype = pages, page_tokens, heads, head_dim, dtype
         self._dev = torch.zeros(size, dtype=torch.uint8, device=device)
         bf16 = dtype == torch.bfloat16

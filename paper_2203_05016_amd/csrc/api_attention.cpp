@@ -13,6 +13,16 @@ bool head_dim_ok(int d) { return d == 64 || d == 96 || d == 128; }
 bool page_ok(int p) { return p >= 32 && p <= 1024 && (p & (p - 1)) == 0; }
 float softmax_scale(int head_dim) { return (float)(1.4426950408889634 / std::sqrt((double)head_dim)); }
 
+int check_sizes(int pages, int page_tokens, int heads, int head_dim)
+{
+    if (!page_ok(page_tokens)) return fail(SHFLBW_ERR_BAD_SHAPE, "page_tokens must be a power of two from 32 to 1024");
+    if (!head_dim_ok(head_dim)) return fail(SHFLBW_ERR_BAD_SHAPE, "head_dim must be 64, 96 or 128");
+    if (heads < 1 || heads > 16384 || pages < 1) return fail(SHFLBW_ERR_BAD_SHAPE, "heads must be 1 to 16384, pages 1 or more");
+    if (heads * (head_dim / 32) > 65535) return fail(SHFLBW_ERR_BAD_SHAPE, "more than 65535 blocks of 32 features in all heads");
+    if ((int64_t)pages * page_tokens > INT_MAX) return fail(SHFLBW_ERR_BAD_SHAPE, "more than 2^31 - 1 slots");
+    return SHFLBW_OK;
+}
+
 int check_sequences(const shflbw_kv_cache* c, const shflbw_kv_sequences* s)
 {
     if (!s) return fail(SHFLBW_ERR_NULL_ARG, "sequences is NULL");
@@ -42,10 +52,8 @@ AttnPlan plan_of(const shflbw_kv_cache* c, const shflbw_kv_sequences* s)
 int check_cache(const shflbw_kv_cache* c)
 {
     if (!c || !c->data) return fail(SHFLBW_ERR_NULL_ARG, "cache or its data is NULL");
-    if (!page_ok(c->page_tokens)) return fail(SHFLBW_ERR_BAD_SHAPE, "page_tokens must be a power of two from 32 to 1024");
-    if (!head_dim_ok(c->head_dim)) return fail(SHFLBW_ERR_BAD_SHAPE, "head_dim must be 64, 96 or 128");
-    if (c->heads < 1 || c->heads > 16384 || c->pages < 1) return fail(SHFLBW_ERR_BAD_SHAPE, "heads must be 1 to 16384, pages 1 or more");
-    if ((int64_t)c->pages * c->page_tokens > INT_MAX) return fail(SHFLBW_ERR_BAD_SHAPE, "more than 2^31 - 1 slots");
+    const int rc = check_sizes(c->pages, c->page_tokens, c->heads, c->head_dim);
+    if (rc < 0) return rc;
     if (c->dtype != SHFLBW_F16 && c->dtype != SHFLBW_BF16) return fail(SHFLBW_ERR_BAD_DTYPE, "dtype must be SHFLBW_F16 or SHFLBW_BF16");
     if (reinterpret_cast<uintptr_t>(c->data) % 128) return fail(SHFLBW_ERR_BAD_SHAPE, "the cache's data must be 128-byte aligned");
     return SHFLBW_OK;
@@ -58,7 +66,7 @@ extern "C" {
 size_t shflbw_kv_cache_bytes(int pages, int page_tokens, int heads, int head_dim)
 {
     using namespace shflbw;
-    if (pages < 1 || heads < 1 || !page_ok(page_tokens) || !head_dim_ok(head_dim)) return 0;
+    if (check_sizes(pages, page_tokens, heads, head_dim) < 0) return 0;
     return (size_t)pages * (size_t)heads * (size_t)page_head_bytes(page_tokens, head_dim);
 }
 

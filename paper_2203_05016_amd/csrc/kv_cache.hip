@@ -121,7 +121,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvArgs a)
 int launch_kv(bool write, const shflbw_kv_cache* c, const KvArgs& a, hipStream_t stream)
 {
     const int64_t blocks = (a.tokens + 255) / 256, parts = (int64_t)a.heads * (c->head_dim / 32);
-    if (blocks > 0x7fffffffLL || parts > 65535) return fail(SHFLBW_ERR_BAD_SHAPE, "grid too large");
+    if (blocks > 0x7fffffffLL) return fail(SHFLBW_ERR_BAD_SHAPE, "grid too large");   // (check_cache: parts are at most 65535)
     const dim3 grid((unsigned)blocks, (unsigned)parts, 2);
     typedef void (*kernel)(KvArgs);
     static const kernel table[2][2][3] = {

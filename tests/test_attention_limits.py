@@ -4,8 +4,9 @@ import os
 import subprocess
 
 import pytest
+import torch
 
-from paper_2203_05016_amd import build as lib_build
+from paper_2203_05016_amd import binding, build as lib_build
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 NONE = 2 ** 31 - 1       # no window
@@ -64,3 +65,20 @@ def test_more_workgroups_than_a_launch_takes_are_counted_as_such(probe):
     for batch, heads, group, tokens in ((1, 1, 65535, 2 ** 31 - 1), (2 ** 31 - 1, 16384, 3, 2 ** 31 - 1), (1000, 16384, 4, 2 ** 31 - 1)):
         probe.probe_cache_blocks(batch, heads, group, 128, tokens, 2 ** 31 - 1, 5000, out)
         assert out[1] > 2 ** 31 - 1 and out[0] > 0, list(out)
+
+
+@pytest.mark.parametrize("pages,page,heads,D", [(1, 32, 16384, 128), (1, 32, 16385, 64), (1, 32, 20000, 96), (1 << 21, 1024, 1, 64), (1 << 26, 32, 1, 64)])
+def test_caches_that_no_call_takes_have_no_size(pages, page, heads, D):
+    """shflbw_kv_cache_bytes gives 0 for what the calls refuse, before memory is laid out for it, and the calls say why."""
+    L = binding.lib()
+    assert L.shflbw_kv_cache_bytes(pages, page, heads, D) == 0
+    cache = binding._Cache(128, pages, page, heads, D, binding.F16)
+    assert L.shflbw_kv_write(cache, 1, 9, 1, 9, 1, 9, None) == -2 and ("heads" if heads > 1 else "slots") in binding.last_error()
+    with pytest.raises(ValueError, match="heads" if heads > 1 else "slots"):
+        binding.KVCache(pages, page, heads, D, torch.float16)
+
+
+def test_the_largest_caches_have_one():
+    size = binding.lib().shflbw_kv_cache_bytes
+    assert size(1, 32, 16384, 64) == 16384 * 32 * 68 and size(1, 32, 16383, 128) == 16383 * 32 * 136
+    assert size((1 << 21) - 1, 1024, 1, 64) == ((1 << 21) - 1) * 1024 * 68
