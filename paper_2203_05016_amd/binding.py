@@ -580,7 +580,8 @@ def window_attention(q, k, v, head_dim, starts=None, max_tokens=None, window=0, 
     """Causal attention of prompts to themselves: q (q_heads * head_dim, tokens), k and v (heads * head_dim, tokens).
 
     Sequence b is columns ``starts[b]`` to ``starts[b + 1] - 1`` (int32, on the GPU); without starts all columns are one.
-    max_tokens: at least the longest sequence's tokens (all of them by default).  A key at j is visible from p if
+    max_tokens: at least the longest sequence's tokens (all of them by default; workgroups are laid out for that many of every
+    sequence, so name it where there are many).  A key at j is visible from p if
     j <= p and (window 0, or p - j < window, or j < sinks)."""
     if stream is None and (_calls or calls()):
         r = _calls.window_attention(q, k, v, head_dim, starts, max_tokens, window, sinks, out)   # None: not the plain case

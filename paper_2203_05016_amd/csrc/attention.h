@@ -62,12 +62,14 @@ struct AttnArgs {
     int col_blocks;           // blocks of columns of a sequence and key head
 };
 
-// Wavefronts per SIMD of the decoding kernel: as many as its registers allow without spilling
+// Wavefronts per SIMD of the decoding kernel that the plan counts on.  Its registers allow no more, but for heads of 64 with 32 and 48
+// columns, which compile to 119 and 155: 4 and 3 would fit.
 SHFLBW_HD constexpr int decode_residency(int col_tiles, int D) { return col_tiles == 1 ? 4 : col_tiles == 2 && D < 128 ? 3 : col_tiles == 4 && D == 128 ? 1 : 2; }
 // Of the other; where it is 3, a CU holds three workgroups of 4 wavefronts: two prompts of 16384 under a window of 1024, 16 heads of 64 take
 // 302 us in these, 340 in workgroups of 8, of which it holds one, 329 in two of 4.  Of 4 for heads of 128 the LDS holds one.
 SHFLBW_HD constexpr int tile_residency(int D, bool cache, int waves) { return waves == 4 && D == 128 ? 1 : waves == 4 && D == 64 && !cache ? 3 : 2; }
-// Rows of a join up to which a row has a workgroup: calls with 128 rows of 32 parts take 52.2 us with it, 54.0 without, with 4096 of 8 30.5 and 27.1
+// Rows of a join up to which a row has a workgroup: calls with 128 rows of 32 parts take 52.2 us with it, 54.0 without, with 4096 of 8 30.5 and 27.1 (between
+// these nothing was measured)
 constexpr int ATTN_FEW_ROWS = 2048;
 constexpr int ATTN_DECODE_KEYS = 32;     // keys of a tile of the decoding kernel
 constexpr int ATTN_TILE_KEYS = 64;       // keys of a tile of the other

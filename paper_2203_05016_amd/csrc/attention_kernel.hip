@@ -194,7 +194,7 @@ __device__ __forceinline__ float attn_max3(float a, float b, float c) { return f
 //
 // Measured: 64 sequences of 819 to 4096 keys, 64 query heads over 8 of 128 (bf16), 189 MB: 40 us, 4.7 TB/s, where a large copy moves 5.1;
 // 2 of 131071 keys (f16, 277 MB) 48 us, 5.8 TB/s (part of it lies in the memory-side cache), and 4.2 for the join; 128 under a window of
-// 1024 with 4 sinks, 16 heads of 64, 144 MB: 30 us, 4.7 TB/s.  Vector instructions are issued in 31 % of the cycles, the matrix units busy in 10.
+// 1024 with 4 sinks, 16 heads of 64, 144 MB: 30 us, 4.7 TB/s.  Vector instructions are issued in 32 % of the cycles, the matrix units busy in 10.
 // With 5 queries each (48 columns; 24 sequences of up to 3001 keys, 56 MB) 34 us: a CU has 8 wavefronts, half of the CUs none.
 template <bool BF, int D, int NT, int W>
 __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_decode_kernel(AttnArgs a)
@@ -494,9 +494,11 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
 // the latter while the former run.  32 queries a wavefront: with 64 the accumulators and two sets of scores and weights are 400 registers, moved
 // and spilled, and the rate is 215 to 690 TFLOP/s.
 //
-// Measured: 4 sequences of 5400 to 9000 keys, 1024 queries each of 64 heads over 8 of 128 (bf16) 917 us, 1.12 PFLOP/s of the 1.26 of a large
-// matrix product; 4 prompts of up to 4096 tokens such 1050 us, 875 TFLOP/s; 2 of 16384 under a window of 1024, 16 heads of 64 (f16) 254 us, 526.  Bound
-// by issue: matrix units are busy in 52, 44 and 30 % of the cycles, vector instructions issued in 53, 48 and 65 %, the clock falls to 1.9 GHz.
+// Measured: 4 sequences of 5400 to 9000 keys, 1024 queries each of 64 heads over 8 of 128 (bf16) 893 us, 1.15 PFLOP/s of the 1.26 of a large
+// matrix product; 4 prompts of up to 4096 tokens such 1023 us, 898 TFLOP/s; 2 of 16384 under a window of 1024, 16 heads of 64 (f16) 252 us, 530.  Matrix
+// units are busy in 52, 44 and 30 % of the cycles, vector instructions issued in 53, 48 and 65 %; the clock is at 2.1 GHz (1.8 in the first dozen
+// launches after a pause, which take up to 18 % longer).  Prompts are further from their floor than chunks: half as many tiles a workgroup, so that first loads and
+// last stores weigh more, and heads of 128 in workgroups of 8 spill 74 registers (300 bytes a lane), which chunks do not.
 //
 // Infinities and NaN among the values of a tile that not all of the workgroup's queries see whole are zeros in the LDS, so that
 // they do not reach a query that does not see them as 0 * NaN; if there were any, they are added where they are seen at the end.  In tiles that all

@@ -68,6 +68,8 @@ AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t to
     const int64_t base = product(pairs, col_blocks);
     // tiles of the longest sequence: window and sinks each may begin inside a tile
     const int64_t tiles = keys_seen(max_length, window, sinks, max_queries) / tile + 3;
+    // One cut for all sequences, by max_length.  Where that is the table's capacity, parts past a sequence's keys have no work: one of 30000 keys, 64
+    // heads over 8 of 128, 16.3 us cut by its length and 24.6 by a table of 131072; 16 of 3000 on average 20.1 and 30.7 by one of 32768.
     // Keys are cut into parts where workgroups are few, into as many as fill the GPU once (what is left over costs a whole round: 24
     // sequences of 3000 keys, 8 heads of 128, 5 queries of 64 heads 48 us in 3 parts of 4 wavefronts, 41 in 2).  The join takes 4
     // to 5 us, so parts are not worth it under twice their least length.
@@ -88,7 +90,7 @@ AttnPlan plan_prompt(int sequences, int heads, int group, int D, int64_t max_tok
     const int64_t items = ceil_div(max_tokens, ATTN_TILE_QUERIES) * group, pairs = (int64_t)sequences * heads;
     // Workgroups of 8 wavefronts share what they bring to the LDS; of 4 where 8 leave CUs without work, for heads of 64 (tile_residency), and
     // for heads of 96, of which a CU holds two, where their keys are few: 8 prompts of 4096, 8 heads, windows of 64, 512 and 1024 61, 99 and 147 us
-    // in these, 70, 114 and 152 in workgroups of 8; without a window, 4 of up to 4096, 32 over 8 heads, 487 and 452.
+    // in these, 70, 114 and 152 in workgroups of 8; without a window, 4 of up to 4096, 32 over 8 heads, 487 and 452 (the bound of 1536 keys lies between).
     const bool few_keys = keys_seen(max_tokens, window, sinks, 0) < 1536;
     // Fewer than 64 columns: in workgroups of 4.
     p.waves = !p.tiny && D > 64 && !(D == 96 && few_keys) && product(ceil_div(items, 8), pairs) >= CUS ? 8 : 4;
