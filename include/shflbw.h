@@ -260,6 +260,41 @@ int shflbw_layernorm_transpose(const void* x, int64_t ldx, const void* gamma, co
                                int K, shflbw_dtype dtype, void* stream);
 
 /*
+ * Queries and keys as attention takes them: every head's column divided by the root of
+ * its mean square, times weights, then turned by its position, in one pass.
+ *
+ *     y = x / sqrt(mean(x^2) + eps) * weight                  (norm; per head and token)
+ *     (a, b) -> (a cos t - b sin t, a sin t + b cos t),       t = position * frequency
+ *
+ * for the pairs (a, b) of the first 2 * pairs features: features i and i + pairs, or
+ * (interleaved) 2 i and 2 i + 1.  The others are not turned.
+ *  head_dim     64, 96 or 128;  pairs 0 to head_dim / 2
+ *  frequencies  device, pairs binary64 numbers: radians per step of the position
+ *  axes         device, pairs: which row of positions each pair goes by (images have one for
+ *               height and one for width).  NULL: the first.  Pairs of a row that is not there become NaN.
+ *  norm         0: turned only (eps, q_weight and k_weight ignored)
+ *  q_weight, k_weight  device, head_dim values of dtype, the same for all heads; NULL: 1.  eps >= 0.
+ * The struct is host memory; what it points to is device memory.
+ */
+typedef struct {
+    int32_t head_dim, dtype, pairs, interleaved, norm, position_rows;
+    double eps;
+    const double* frequencies;
+    const int32_t* axes;
+    const void *q_weight, *k_weight;
+} shflbw_rotation;
+
+/* Turns q (device, q_heads * head_dim x tokens of dtype, tokens innermost) and k (heads * head_dim x tokens; heads may be
+ * 0, and k NULL) into q_out and k_out.
+ *  positions  device, position_rows x tokens (leading dimension ldp >= tokens), of either sign; NULL where pairs is 0
+ *  q_out, k_out  the same memory and leading dimension as q and k (in place), or memory that overlaps neither.
+ * Angles are worked out in binary64, everything else in binary32 (squares that binary32 does not hold in binary64), rounded to dtype
+ * once.  Any alignment.  tokens == 0 is a no-op.  Enqueues on `stream` only. */
+int shflbw_norm_rotate(const shflbw_rotation* rotation, const int32_t* positions, int64_t ldp, const void* q, int64_t ldq, int q_heads,
+                       const void* k, int64_t ldk, int heads, void* q_out, int64_t ldqo, void* k_out, int64_t ldko, int64_t tokens,
+                       void* stream);
+
+/*
  * Cache of keys and values in 4 bits, in pages, for serving.  Activations are
  * features x tokens with the tokens innermost, as shflbw_spmm takes and leaves
  * them; head h owns rows h * head_dim and up.
@@ -353,6 +388,88 @@ int shflbw_kv_attention(const shflbw_kv_cache* cache, const shflbw_kv_sequences*
                         void* out, int64_t ldo, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
+ * The prefixes of a shflbw_kv_shared_attention call: tokens at the front of several sequences that the cache holds once.
+ *  prefixes    how many
+ *  table       device, prefixes x table_pages pages (leading dimension table_ld), as that of the sequences
+ *  lengths     device, prefixes: tokens of each; 0 is a prefix of nothing.  Beyond table_pages pages: NaN.
+ *  members     device, prefixes + 1: prefix g is that of sequences members[g] to members[g + 1] - 1, whose columns follow each
+ *              other.  NULL: one prefix, of all sequences.  Columns of sequences of no prefix are left undefined.
+ *  max_length  the longest prefix's tokens, as far as the host knows them: decides how the work is cut only, as the sequences' does
+ *  max_tokens  at least the columns of q that any prefix's sequences have together: columns past it are left undefined
+ */
+typedef struct {
+    int32_t prefixes, table_pages;
+    int64_t table_ld, max_length, max_tokens;
+    const int32_t *table, *lengths, *members;
+} shflbw_kv_prefixes;
+
+/* Bytes of device workspace that shflbw_kv_shared_attention needs (the pointers of the structs are not followed), or a negative status. */
+int64_t shflbw_kv_shared_attention_workspace(const shflbw_kv_cache* cache, const shflbw_kv_prefixes* prefixes, const shflbw_kv_sequences* sequences);
+
+/*
+ * Attention over the cache of sequences that share prefixes: every query sees all tokens of its sequence's prefix, and its
+ * sequence's own tokens up to its own position, as in shflbw_kv_attention, whose table, lengths and
+ * positions are the own tokens' alone (a length of 0, or below the queries, leaves queries with the prefix).  A prefix is read once for
+ * all queries of all its sequences.  window must be 0 (under a window a far prefix is not seen: shflbw_kv_attention takes its pages
+ * in the sequence's table).  Columns of q before the first sequence's and behind the last one's are left as they were.
+ * A workspace is always needed; everything else, accuracy included, is as in shflbw_kv_attention.
+ */
+int shflbw_kv_shared_attention(const shflbw_kv_cache* cache, const shflbw_kv_prefixes* prefixes, const shflbw_kv_sequences* sequences,
+                               const void* q, int64_t ldq, void* out, int64_t ldo, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Which pages belong to which sequences, on the device, so that a captured step can hand out and give back pages.
+ *  sequences, table_pages  rows and columns of the table
+ *  table    device, sequences x table_pages (leading dimension table_ld).  Row b's first ceil(lengths[b] / page_tokens) entries are
+ *           its pages (at most table_pages); the others are not looked at, and are -1 in tables that a call writes.
+ *  lengths  device, sequences: tokens.  Below 0 is taken as 0.
+ *  uses     device, one count for each of the cache's pages: how many entries of tables name it.  A page is free where that is 0.
+ * Entries outside the cache are kept and name no page.  Free pages are taken from the lowest up.  Where there are none left, the entry
+ * becomes -1 (such a page reads as NaN, and its slots are skipped by shflbw_kv_write); its tokens count as the sequence's all the same.
+ * Results depend on the arguments alone, not on the order of anything on the device.  The structs are host memory.
+ */
+typedef struct {
+    int32_t sequences, table_pages;
+    int64_t table_ld;
+    int32_t *table, *lengths, *uses;
+} shflbw_kv_pages;
+
+/* Bytes of device workspace that the three calls below need, or a negative status. */
+int64_t shflbw_kv_pages_workspace(const shflbw_kv_cache* cache, int sequences);
+
+/*
+ * More tokens for every sequence: sequence b gets counts[b] (device; below 0 is none), the pages it lacks for them, in order of
+ * sequence and position, and their slots.
+ *  in, out  of one shape; every array of out is the same as in's (in place) or overlaps none of them
+ *  slots    device, tokens: the slots of the new tokens, sequence after sequence, to be written to; -1 where there is no page, and
+ *           past the last token.  Tokens past `tokens` have no slot.
+ *  starts   device, sequences + 1: where each sequence's begin (shflbw_kv_sequences.starts of their queries)
+ * Lengths and starts stop at 2^31 - 1.  A last page that is not yet full must not be shared (shflbw_kv_fork leaves none that is).
+ */
+int shflbw_kv_extend(const shflbw_kv_cache* cache, const shflbw_kv_pages* in, const shflbw_kv_pages* out, const int32_t* counts,
+                     int32_t* slots, int32_t* starts, int64_t tokens, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Sequences that continue others: row i of out gets the tokens of row parents[i] of in (device, out->sequences; a number outside
+ * in's rows leaves row i without tokens).  Full pages are shared.  A last page that is not full is kept by the
+ * lowest i that continues its row, and copied whole to a free page for every other.  Rows that nothing continues are given up: pages that no
+ * table names any more are free, and may be taken by this call's copies.
+ *  in, out  of the same table_pages; no array of out overlaps one of in, but uses, which may be the same
+ * uses may count entries of other tables too; such pages stay.
+ */
+int shflbw_kv_fork(const shflbw_kv_cache* cache, const shflbw_kv_pages* in, const shflbw_kv_pages* out, const int32_t* parents,
+                   void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The pages in use to the front of the cache: with n pages in use, those from n on move, in ascending order, to the free ones
+ * below n, in ascending order, contents and counts; entries of the table that name them (all table_pages columns) follow.  Lengths are
+ * neither read nor written (NULL will do).  Every table that is used any further has to be part of this one.
+ *  in, out  of one shape; every array of out is the same as in's (in place) or overlaps none of them
+ */
+int shflbw_kv_compact(const shflbw_kv_cache* cache, const shflbw_kv_pages* in, const shflbw_kv_pages* out, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+
+/*
  * Attention of prompts to themselves, causal, with an optional sliding window
  * and first tokens (sinks) that stay visible; keys and values in 16 bits.
  *  q, out  device, q_heads * head_dim x tokens of dtype; k, v: heads * head_dim
@@ -376,7 +493,7 @@ const char* shflbw_status_string(int status);
 const char* shflbw_last_error(void); /* thread-local, never NULL */
 
 /* Which kernel the calling thread's most recent successful shflbw_spmm, shflbw_conv2d,
- * shflbw_kv_attention or shflbw_window_attention launched, as "name<template arguments>" (the automatic choice of set_tuning(0, 0) is
+ * shflbw_kv_attention, shflbw_kv_shared_attention (the prefixes' kernel) or shflbw_window_attention launched, as "name<template arguments>" (the automatic choice of set_tuning(0, 0) is
  * made per call from the matrix and the operand shape).  Thread-local, never NULL; empty
  * before the first launch. */
 const char* shflbw_last_kernel(void);

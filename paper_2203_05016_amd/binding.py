@@ -27,7 +27,9 @@ EXPORTS = [
     "shflbw_set_tuning", "shflbw_device_status", "shflbw_set_wait_limit", "shflbw_spmm", "shflbw_spmm_unbound",
     "shflbw_conv2d",
     "shflbw_layernorm_transpose", "shflbw_kv_cache_bytes", "shflbw_kv_write", "shflbw_kv_read",
-    "shflbw_kv_attention_workspace", "shflbw_kv_attention", "shflbw_window_attention", "shflbw_status_string", "shflbw_last_error", "shflbw_last_kernel",
+    "shflbw_kv_attention_workspace", "shflbw_kv_attention", "shflbw_window_attention",
+    "shflbw_norm_rotate", "shflbw_kv_shared_attention_workspace", "shflbw_kv_shared_attention", "shflbw_kv_pages_workspace",
+    "shflbw_kv_extend", "shflbw_kv_fork", "shflbw_kv_compact", "shflbw_status_string", "shflbw_last_error", "shflbw_last_kernel",
 ]
 
 
@@ -46,6 +48,23 @@ class _Sequences(ctypes.Structure):   # shflbw_kv_sequences
     _fields_ = [(name, ctypes.c_int32) for name in ("q_heads", "batch", "max_queries", "table_pages", "window", "sinks")] + \
                [(name, ctypes.c_int64) for name in ("tokens", "max_length", "table_ld")] + \
                [(name, ctypes.c_void_p) for name in ("table", "lengths", "starts")]
+
+
+class _Prefixes(ctypes.Structure):   # shflbw_kv_prefixes
+    _fields_ = [(name, ctypes.c_int32) for name in ("prefixes", "table_pages")] + \
+        [(name, ctypes.c_int64) for name in ("table_ld", "max_length", "max_tokens")] + \
+        [(name, ctypes.c_void_p) for name in ("table", "lengths", "members")]
+
+
+class _Pages(ctypes.Structure):   # shflbw_kv_pages
+    _fields_ = [(name, ctypes.c_int32) for name in ("sequences", "table_pages")] + [("table_ld", ctypes.c_int64)] + \
+        [(name, ctypes.c_void_p) for name in ("table", "lengths", "uses")]
+
+
+class _Rotation(ctypes.Structure):   # shflbw_rotation
+    _fields_ = [(name, ctypes.c_int32) for name in ("head_dim", "dtype", "pairs", "interleaved", "norm", "position_rows")] + \
+        [("eps", ctypes.c_double)] + [(name, ctypes.c_void_p) for name in ("frequencies", "axes", "q_weight", "k_weight")]
+
 
 
 def lib():
@@ -104,6 +123,21 @@ def lib():
         L.shflbw_kv_attention.argtypes = [cache, sequences, vp, i64, vp, i64, vp, i64, vp]
         L.shflbw_window_attention.restype = i32
         L.shflbw_window_attention.argtypes = [vp, i64] * 4 + [i32, i32, i32, i64, vp, i32, i64, i32, i32, i32, vp]
+        prefixes, pages, rotation = ctypes.POINTER(_Prefixes), ctypes.POINTER(_Pages), ctypes.POINTER(_Rotation)
+        L.shflbw_norm_rotate.restype = i32
+        L.shflbw_norm_rotate.argtypes = [rotation, vp, i64, vp, i64, i32, vp, i64, i32, vp, i64, vp, i64, i64, vp]
+        L.shflbw_kv_shared_attention_workspace.restype = i64
+        L.shflbw_kv_shared_attention_workspace.argtypes = [cache, prefixes, sequences]
+        L.shflbw_kv_shared_attention.restype = i32
+        L.shflbw_kv_shared_attention.argtypes = [cache, prefixes, sequences, vp, i64, vp, i64, vp, i64, vp]
+        L.shflbw_kv_pages_workspace.restype = i64
+        L.shflbw_kv_pages_workspace.argtypes = [cache, i32]
+        L.shflbw_kv_extend.restype = i32
+        L.shflbw_kv_extend.argtypes = [cache, pages, pages, vp, vp, vp, i64, vp, i64, vp]
+        L.shflbw_kv_fork.restype = i32
+        L.shflbw_kv_fork.argtypes = [cache, pages, pages, vp, vp, i64, vp]
+        L.shflbw_kv_compact.restype = i32
+        L.shflbw_kv_compact.argtypes = [cache, pages, pages, vp, i64, vp]
         L.shflbw_status_string.restype = ctypes.c_char_p
         L.shflbw_status_string.argtypes = [i32]
         L.shflbw_last_error.restype = ctypes.c_char_p
@@ -468,6 +502,27 @@ def _natural(**numbers):
             raise ValueError("%s must be a whole number from 0 to 2^31 - 1, got %r" % (name, n))
 
 
+def _table(t, name):
+    """Checks a (rows, pages) table; returns its leading dimension."""
+    import torch
+    if t.dtype != torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or t.shape[1] < 1:
+        raise TypeError("%s must be a 2-D int32 tensor with unit page stride and a page or more" % name)
+    rows, width = t.shape
+    if rows > 1 and t.stride(0) < width:
+        raise ValueError("rows of %s overlap" % name)
+    return t.stride(0) if rows > 1 else width
+
+
+def _launch_on(device, stream):
+    """The context and the stream's handle for a launch on `device`: kernels start on the current GPU, and torch's current stream is that GPU's."""
+    import contextlib
+    import torch
+    if stream is not None and stream.device != device:
+        raise ValueError("the stream is %s's, the tensors live on %s" % (stream.device, device))
+    on = contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    return on, (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+
+
 class KVCache:
     """Keys and values of many sequences in 4 bits, in pages on a GPU (the format is shflbw_kv_cache's).
 
@@ -496,6 +551,11 @@ class KVCache:
     @property
     def device(self):
         return self._dev.device
+
+    @property
+    def data(self):
+        """The cache's bytes, (pages, bytes of a page): whole pages can be copied, kept elsewhere and brought back."""
+        return self._dev.view(self.pages, -1)
 
     def device_bytes(self):
         return self._dev.numel()
@@ -574,6 +634,195 @@ class KVCache:
         _check(lib().shflbw_kv_attention(self._c, s, q.data_ptr(), ldq, out.data_ptr(), ldo, work.data_ptr() if size else None, size,
                                          _stream_ptr(stream)))
         return out
+
+    def shared_attention(self, q, prefix_table, prefix_lengths, table, lengths, members=None, starts=None, max_queries=1, max_length=None,
+                         max_prefix=None, max_sharing=None, out=None, stream=None):
+        """Attention of sequences that share prefixes, each of which is read once for all of them.
+
+        q, table, lengths, starts, max_queries and max_length are those of ``attention``, the table and lengths those of the sequences' own tokens: every query
+        sees its prefix whole, and its sequence's own tokens up to its own.  prefix_table (prefixes, pages) and prefix_lengths (prefixes,)
+        int32: the prefixes' pages and tokens.  members (prefixes + 1,) int32: prefix g is that of sequences ``members[g]`` to
+        ``members[g + 1] - 1``; without members one prefix is everybody's.  max_prefix: the longest prefix's tokens (all of the table's pages by
+        default), which decides how the work is cut only.  max_sharing: at least the columns of q that any prefix's sequences have
+        together (all of them by default)."""
+        import torch
+        if q.dtype != self.dtype or q.dim() != 2 or q.shape[0] == 0 or q.shape[0] % (self.heads * self.head_dim):
+            raise TypeError("q must be a 2-D %s tensor with a multiple of %d rows" % (self.dtype, self.heads * self.head_dim))
+        rows, tokens = q.shape
+        ldq = _columns(q, "q", rows, self.dtype)
+        ld, prefix_ld = _table(table, "table"), _table(prefix_table, "prefix_table")
+        (batch, width), (prefixes, prefix_width) = table.shape, prefix_table.shape
+        _indices(lengths, "lengths", batch)
+        _indices(prefix_lengths, "prefix_lengths", prefixes)
+        if members is not None:
+            _indices(members, "members", prefixes + 1)
+        elif prefixes != 1:
+            raise ValueError("without members there is one prefix, got %d" % prefixes)
+        if starts is not None:
+            _indices(starts, "starts", batch + 1)
+        elif tokens != batch or max_queries != 1:
+            raise ValueError("without starts every sequence has one query: q must have %d columns, max_queries be 1" % batch)
+        max_length = width * self.page_tokens if max_length is None else max_length
+        max_prefix = prefix_width * self.page_tokens if max_prefix is None else max_prefix
+        max_sharing = max(tokens, 1) if max_sharing is None else max_sharing
+        _natural(max_queries=max_queries, max_length=max_length, max_prefix=max_prefix, max_sharing=max_sharing)
+        _on(self.device, q=q, prefix_table=prefix_table, prefix_lengths=prefix_lengths, table=table, lengths=lengths, members=members,
+            starts=starts, out=out)
+        on, handle = _launch_on(self.device, stream)
+        if out is None:
+            out = _result((rows, tokens), self.dtype, self.device, stream)
+        ldo = _columns(out, "out", rows, self.dtype, tokens)
+        address = lambda t: None if t is None else t.data_ptr()
+        p = _Prefixes(prefixes, prefix_width, prefix_ld, max_prefix, max_sharing, prefix_table.data_ptr(), prefix_lengths.data_ptr(), address(members))
+        s = _Sequences(rows // self.head_dim, batch, max_queries, width, 0, 0, tokens, max_length, ld, table.data_ptr(), lengths.data_ptr(), address(starts))
+        size = _check(lib().shflbw_kv_shared_attention_workspace(self._c, p, s))
+        work = _empty(size, torch.uint8, self.device, stream)
+        with on:
+            _check(lib().shflbw_kv_shared_attention(self._c, p, s, q.data_ptr(), ldq, out.data_ptr(), ldo, work.data_ptr(), size, handle))
+        return out
+
+    def _held(self, name, table, lengths, uses, out, rows, stream):
+        """Checks tables, lengths (None: there are none) and uses of a call on pages, and makes its results; returns both as shflbw_kv_pages, and the results."""
+        import torch
+        ld = _table(table, "table")
+        width = table.shape[1]
+        if lengths is not None:
+            _indices(lengths, "lengths", table.shape[0])
+        _indices(uses, "uses", self.pages)
+        _on(self.device, table=table, lengths=lengths, uses=uses)
+        if out is None:
+            shapes = [(rows, width)] + ([(rows,)] if lengths is not None else []) + [(self.pages,)]
+            out = tuple(_result(shape, torch.int32, self.device, stream) for shape in shapes)
+        if len(out) != (2 if lengths is None else 3):
+            raise ValueError("out must be %d tensors" % (2 if lengths is None else 3))
+        new_table, new_uses = out[0], out[-1]
+        new_ld = _table(new_table, "the new table")
+        if tuple(new_table.shape) != (rows, width):
+            raise ValueError("the new table must have shape (%d, %d), got %r" % (rows, width, tuple(new_table.shape)))
+        if lengths is not None:
+            _indices(out[1], "the new lengths", rows)
+        _indices(new_uses, "the new uses", self.pages)
+        _on(self.device, **{"out[%d]" % i: t for i, t in enumerate(out)})
+        address = lambda t: None if t is None else t.data_ptr()
+        return (_Pages(table.shape[0], width, ld, table.data_ptr(), address(lengths), uses.data_ptr()),
+                _Pages(rows, width, new_ld, new_table.data_ptr(), address(out[1] if lengths is not None else None), new_uses.data_ptr()), tuple(out))
+
+    def _pages_work(self, sequences, stream):
+        import torch
+        return _empty(_check(lib().shflbw_kv_pages_workspace(self._c, sequences)), torch.uint8, self.device, stream)
+
+    def extend(self, table, lengths, uses, counts, tokens, out=None, slots=None, starts=None, stream=None):
+        """counts[b] more tokens for every sequence: the pages they lack, the lowest free ones, and where to write the tokens.
+
+        table (sequences, pages) int32: the pages of every sequence in order, lengths (sequences,) int32 its tokens, uses (pages of the cache,)
+        int32 how many entries of tables name each page; counts (sequences,) int32.  tokens: how many slots are wanted, at least what
+        counts add up to.  Returns (table, lengths, uses, slots, starts): slots (tokens,) for ``write``, -1 where there is no page left and past the last token,
+        starts (sequences + 1,) for ``attention``.  out: the first three's memory, which may be the arguments' own; slots, starts: theirs."""
+        import torch
+        _natural(tokens=tokens)
+        rows = table.shape[0] if table.dim() else 0
+        before, after, out = self._held("extend", table, lengths, uses, out, rows, stream)
+        _indices(counts, "counts", rows)
+        slots = _result((tokens,), torch.int32, self.device, stream) if slots is None else slots
+        starts = _result((rows + 1,), torch.int32, self.device, stream) if starts is None else starts
+        _indices(slots, "slots", tokens)
+        _indices(starts, "starts", rows + 1)
+        _on(self.device, counts=counts, slots=slots, starts=starts)
+        on, handle = _launch_on(self.device, stream)
+        work = self._pages_work(rows, stream)
+        with on:
+            _check(lib().shflbw_kv_extend(self._c, before, after, counts.data_ptr(), slots.data_ptr(), starts.data_ptr(), tokens, work.data_ptr(),
+                                          work.numel(), handle))
+        return out + (slots, starts)
+
+    def fork(self, table, lengths, uses, parents, out=None, stream=None):
+        """Sequences that continue others: row i of the new table gets the tokens of row ``parents[i]`` (int32; a number that is no row: none).
+
+        Full pages are shared; a last page that is not full is copied to a free one for all but the first that continues its
+        row.  Rows that nothing continues give their pages up.  Returns the new (table, lengths, uses); out: their memory, which
+        must not be the arguments' own but for uses."""
+        rows = parents.shape[0] if parents.dim() else 0
+        _indices(parents, "parents", rows)
+        before, after, out = self._held("fork", table, lengths, uses, out, rows, stream)
+        _on(self.device, parents=parents)
+        on, handle = _launch_on(self.device, stream)
+        work = self._pages_work(max(rows, table.shape[0]), stream)
+        with on:
+            _check(lib().shflbw_kv_fork(self._c, before, after, parents.data_ptr(), work.data_ptr(), work.numel(), handle))
+        return out
+
+    def compact(self, table, uses, out=None, stream=None):
+        """Moves the pages in use to the front of the cache, as few of them as possible: with n in use they are pages 0 to n - 1 afterwards.
+
+        Returns the new (table, uses); out: their memory, which may be the arguments' own.  Every table in use has to be part of this one."""
+        rows = table.shape[0] if table.dim() else 0
+        before, after, out = self._held("compact", table, None, uses, out, rows, stream)
+        on, handle = _launch_on(self.device, stream)
+        work = self._pages_work(rows, stream)
+        with on:
+            _check(lib().shflbw_kv_compact(self._c, before, after, work.data_ptr(), work.numel(), handle))
+        return out
+
+
+def norm_rotate(q, k, head_dim, positions, frequencies, axes=None, q_weight=None, k_weight=None, eps=1e-6, norm=True, interleaved=False,
+                q_out=None, k_out=None, stream=None):
+    """Queries (q_heads * head_dim, tokens) and keys (heads * head_dim, tokens; or None) as attention takes them: every head's column over the root
+    of its mean square (plus eps), times weights (head_dim,), then turned by its position.  norm False: only turned.
+
+    frequencies (pairs,) float64: radians per step of the position for each pair of features, i and i + pairs (interleaved: 2 i and 2 i + 1); the
+    features past 2 * pairs are not turned.  positions (tokens,) or (rows, tokens) int32; axes (pairs,) int32: which row each pair goes by, the first
+    without it.  All on the GPU.  Returns (q, k) of q's dtype; q_out, k_out: their memory, which may be q and k themselves."""
+    import torch
+    if q.dtype not in (torch.float16, torch.bfloat16) or q.dim() != 2:
+        raise TypeError("q must be a 2-D float16 or bfloat16 tensor")
+    _natural(head_dim=head_dim)
+    q_rows, tokens = q.shape
+    k_rows = 0 if k is None else k.shape[0] if k.dim() == 2 else -1
+    if head_dim == 0 or k_rows < 0 or q_rows % head_dim or k_rows % head_dim:
+        raise ValueError("q and k must be 2-D with a multiple of head_dim = %d rows" % head_dim)
+    ldq = _columns(q, "q", q_rows, q.dtype)
+    ldk = 0 if k is None else _columns(k, "k", k_rows, q.dtype, tokens)
+    if frequencies.dtype != torch.float64 or frequencies.dim() != 1 or not frequencies.is_contiguous():
+        raise TypeError("frequencies must be a contiguous 1-D float64 tensor")
+    pairs = frequencies.shape[0]
+    if 2 * pairs > head_dim:
+        raise ValueError("%d frequencies for heads of %d features" % (pairs, head_dim))
+    if positions.dtype != torch.int32 or positions.dim() not in (1, 2) or positions.shape[-1] != tokens or (tokens > 1 and positions.stride(-1) != 1):
+        raise TypeError("positions must be int32, (%d,) or (rows, %d), with unit token stride" % (tokens, tokens))
+    position_rows = positions.shape[0] if positions.dim() == 2 else 1
+    ldp = positions.stride(0) if positions.dim() == 2 and position_rows > 1 else max(tokens, 1)
+    if ldp < tokens:
+        raise ValueError("rows of positions overlap")
+    if position_rows < 1:
+        raise ValueError("positions must have a row or more")
+    if axes is not None:
+        _indices(axes, "axes", pairs)
+    elif position_rows > 1:
+        raise ValueError("positions of %d rows need axes" % position_rows)
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None and not norm:
+            raise ValueError("%s without norm" % name)
+        if w is not None and (w.dtype != q.dtype or tuple(w.shape) != (head_dim,) or not w.is_contiguous()):
+            raise TypeError("%s must be a contiguous (%d,) tensor of q's dtype" % (name, head_dim))
+    if (k is None) and (k_weight is not None or k_out is not None):
+        raise ValueError("k_weight or k_out without k")
+    if not q.is_cuda:
+        raise ValueError("q must live on a GPU (got %s)" % q.device)
+    _on(q.device, k=k, positions=positions, frequencies=frequencies, axes=axes, q_weight=q_weight, k_weight=k_weight, q_out=q_out, k_out=k_out)
+    on, handle = _launch_on(q.device, stream)
+    if q_out is None:
+        q_out = _result((q_rows, tokens), q.dtype, q.device, stream)
+    if k_out is None and k is not None:
+        k_out = _result((k_rows, tokens), q.dtype, q.device, stream)
+    ldqo = _columns(q_out, "q_out", q_rows, q.dtype, tokens)
+    ldko = 0 if k is None else _columns(k_out, "k_out", k_rows, q.dtype, tokens)
+    address = lambda t: None if t is None else t.data_ptr()
+    r = _Rotation(head_dim, BF16 if q.dtype == torch.bfloat16 else F16, pairs, bool(interleaved), bool(norm), position_rows, float(eps),
+                  frequencies.data_ptr(), address(axes), address(q_weight), address(k_weight))
+    with on:
+        _check(lib().shflbw_norm_rotate(r, positions.data_ptr(), ldp, q.data_ptr(), ldq, q_rows // head_dim, address(k), ldk, k_rows // head_dim,
+                                        q_out.data_ptr(), ldqo, address(k_out), ldko, tokens, handle))
+    return q_out, k_out
 
 
 def window_attention(q, k, v, head_dim, starts=None, max_tokens=None, window=0, sinks=0, out=None, stream=None):

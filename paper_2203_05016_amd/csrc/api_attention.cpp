@@ -47,6 +47,52 @@ AttnPlan plan_of(const shflbw_kv_cache* c, const shflbw_kv_sequences* s)
                                 s->window ? s->window : INT_MAX, s->sinks);
 }
 
+int check_prefixes(const shflbw_kv_cache* c, const shflbw_kv_prefixes* p, const shflbw_kv_sequences* s)
+{
+    if (!p) return fail(SHFLBW_ERR_NULL_ARG, "prefixes is NULL");
+    if (s->window || s->sinks) return fail(SHFLBW_ERR_BAD_SHAPE, "shared prefixes are seen whole: window and sinks must be 0");
+    if (p->prefixes < 1 || (!p->members && p->prefixes != 1)) return fail(SHFLBW_ERR_BAD_SHAPE, "prefixes must be 1 or more, and 1 without members");
+    if (p->table_pages < 1 || p->table_ld < p->table_pages) return fail(SHFLBW_ERR_BAD_SHAPE, "table_pages < 1 or table_ld < table_pages (prefixes)");
+    if ((int64_t)p->table_pages * c->page_tokens > INT_MAX - 1024) return fail(SHFLBW_ERR_BAD_SHAPE, "more than 2^31 tokens in a prefix's pages");
+    if (p->max_length < 1 || p->max_length > (int64_t)p->table_pages * c->page_tokens)
+        return fail(SHFLBW_ERR_BAD_SHAPE, "max_length must lie between 1 and the tokens of table_pages pages (prefixes)");
+    if (p->max_tokens < 1) return fail(SHFLBW_ERR_BAD_SHAPE, "max_tokens < 1");
+    return SHFLBW_OK;
+}
+
+SharedPlan plan_of(const shflbw_kv_cache* c, const shflbw_kv_prefixes* p, const shflbw_kv_sequences* s)
+{
+    return plan_shared_attention(p->prefixes, p->max_tokens, p->max_length, s->batch, c->heads, s->q_heads / c->heads, c->head_dim, s->tokens, s->max_queries,
+                                 s->max_length);
+}
+
+// What a call over the cache gives the kernels, but for where results go
+AttnArgs cache_args(const shflbw_kv_cache* c, const shflbw_kv_sequences* s, const AttnPlan& plan, const void* q, int64_t ldq)
+{
+    AttnArgs a = {};
+    a.q = static_cast<const uint16_t*>(q);
+    a.cache = static_cast<const char*>(c->data);
+    a.table = s->table;
+    a.lengths = s->lengths;
+    a.starts = s->starts;
+    a.ldq = ldq;
+    a.table_ld = s->table_ld;
+    a.tokens = s->tokens;
+    a.table_width = s->table_pages;
+    a.batch = s->batch;
+    a.heads = c->heads;
+    a.group = s->q_heads / c->heads;
+    a.pages = c->pages;
+    a.page_shift = __builtin_ctz(c->page_tokens);
+    a.window = s->window ? s->window : INT_MAX;
+    a.sinks = s->sinks;
+    a.scale = softmax_scale(c->head_dim);
+    a.splits = plan.splits;
+    a.split_tiles = plan.split_tiles;
+    a.col_blocks = plan.col_blocks;
+    return a;
+}
+
 }  // namespace
 
 int check_cache(const shflbw_kv_cache* c)
@@ -91,32 +137,56 @@ int shflbw_kv_attention(const shflbw_kv_cache* cache, const shflbw_kv_sequences*
     if (plan.workspace > workspace_bytes || (plan.workspace && !workspace))
         return fail(SHFLBW_ERR_NULL_ARG, "the call needs a workspace of %lld bytes", (long long)plan.workspace);
     if (plan.workspace && reinterpret_cast<uintptr_t>(workspace) % 16) return fail(SHFLBW_ERR_BAD_SHAPE, "the workspace must be 16-byte aligned");
-    AttnArgs a = {};
-    a.q = static_cast<const uint16_t*>(q);
-    a.cache = static_cast<const char*>(cache->data);
-    a.table = s->table;
-    a.lengths = s->lengths;
-    a.starts = s->starts;
+    AttnArgs a = cache_args(cache, s, plan, q, ldq);
     a.out = static_cast<uint16_t*>(out);
-    a.part_o = static_cast<float*>(workspace);
-    a.part_ml = a.part_o + (int64_t)plan.splits * s->q_heads * s->tokens * cache->head_dim;
-    a.ldq = ldq; a.ldo = ldo;
-    a.table_ld = s->table_ld;
-    a.tokens = s->tokens;
-    a.table_width = s->table_pages;
-    a.batch = s->batch;
-    a.heads = cache->heads;
-    a.group = s->q_heads / cache->heads;
-    a.pages = cache->pages;
-    a.page_shift = __builtin_ctz(cache->page_tokens);
-    a.window = s->window ? s->window : INT_MAX;
-    a.sinks = s->sinks;
-    a.scale = softmax_scale(cache->head_dim);
-    a.splits = plan.splits;
-    a.split_tiles = plan.split_tiles;
-    a.col_blocks = plan.col_blocks;
+    a.ldo = ldo;
+    if (plan.splits > 1) {
+        a.part_o = static_cast<float*>(workspace);
+        a.part_ml = a.part_o + (int64_t)plan.splits * s->q_heads * s->tokens * cache->head_dim;
+    }
     return cache->dtype == SHFLBW_BF16 ? run_attention_bf16(a, plan, cache->head_dim, false, stream)
                                        : run_attention_f16(a, plan, cache->head_dim, false, stream);
+}
+
+int64_t shflbw_kv_shared_attention_workspace(const shflbw_kv_cache* cache, const shflbw_kv_prefixes* prefixes, const shflbw_kv_sequences* sequences)
+{
+    using namespace shflbw;
+    int rc = check_cache(cache);
+    if (rc < 0 || (rc = check_sequences(cache, sequences)) < 0 || (rc = check_prefixes(cache, prefixes, sequences)) < 0) return rc;
+    return sequences->batch ? plan_of(cache, prefixes, sequences).workspace : 0;
+}
+
+int shflbw_kv_shared_attention(const shflbw_kv_cache* cache, const shflbw_kv_prefixes* prefixes, const shflbw_kv_sequences* s, const void* q, int64_t ldq,
+                               void* out, int64_t ldo, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    using namespace shflbw;
+    int rc = check_cache(cache);
+    if (rc < 0 || (rc = check_sequences(cache, s)) < 0 || (rc = check_prefixes(cache, prefixes, s)) < 0) return rc;
+    if (s->batch == 0 || s->tokens == 0) return SHFLBW_OK;
+    if (!q || !out || !s->table || !s->lengths || !prefixes->table || !prefixes->lengths)
+        return fail(SHFLBW_ERR_NULL_ARG, "q, out, tables and lengths must not be NULL");
+    if (ldq < s->tokens || ldo < s->tokens) return fail(SHFLBW_ERR_BAD_SHAPE, "leading dimension too small");
+    const SharedPlan plan = plan_of(cache, prefixes, s);
+    if (plan.workspace > workspace_bytes || !workspace) return fail(SHFLBW_ERR_NULL_ARG, "the call needs a workspace of %lld bytes", (long long)plan.workspace);
+    if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(SHFLBW_ERR_BAD_SHAPE, "the workspace must be 16-byte aligned");
+    const int64_t rows = (int64_t)s->q_heads * s->tokens, parts = plan.prefix.splits + plan.own.splits;
+    AttnArgs own = cache_args(cache, s, plan.own, q, ldq), prefix = cache_args(cache, s, plan.prefix, q, ldq);
+    prefix.table = prefixes->table;
+    prefix.lengths = prefixes->lengths;
+    prefix.table_ld = prefixes->table_ld;
+    prefix.table_width = prefixes->table_pages;
+    prefix.batch = prefixes->prefixes;
+    prefix.shared = true;
+    prefix.members = prefixes->members;
+    prefix.sequences = s->batch;
+    prefix.out = own.out = static_cast<uint16_t*>(out);
+    prefix.ldo = own.ldo = ldo;
+    prefix.part_o = static_cast<float*>(workspace);
+    prefix.part_ml = prefix.part_o + parts * rows * cache->head_dim;
+    own.part_o = prefix.part_o + plan.prefix.splits * rows * cache->head_dim;
+    own.part_ml = prefix.part_ml + 2 * plan.prefix.splits * rows;
+    return cache->dtype == SHFLBW_BF16 ? run_shared_attention_bf16(prefix, own, plan, cache->head_dim, stream)
+                                       : run_shared_attention_f16(prefix, own, plan, cache->head_dim, stream);
 }
 
 int shflbw_window_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, void* out, int64_t ldo,

@@ -49,7 +49,7 @@ struct AttnArgs {
     const int32_t* lengths;   // cached tokens of every sequence
     const int32_t* starts;    // first query of every sequence and the end; nullptr: one query each (prompt: one sequence)
     uint16_t* out;
-    float* part_o;            // splits > 1: [split][q_head][token][D] sums that are not divided yet ..
+    float* part_o;            // nullptr: out takes the results.  Otherwise [split][q_head][token][D] sums that are not divided yet ..
     float* part_ml;           // .. and [split][q_head][token][2], their maximum and sum of weights
     int64_t ldq, ldk, ldv, ldo, table_ld;
     int64_t tokens;           // columns of q
@@ -60,6 +60,10 @@ struct AttnArgs {
     float scale;              // log2(e) / sqrt(D)
     int splits, split_tiles;  // parts a sequence's keys are cut into, key tiles of a part
     int col_blocks;           // blocks of columns of a sequence and key head
+    // Prefixes: a "sequence" is a prefix, whose queries are those of sequences members[b] to members[b + 1] - 1 (nullptr: of all) and see all of its keys
+    bool shared;
+    const int32_t* members;
+    int sequences;            // of `starts`
 };
 
 // Wavefronts per SIMD of the decoding kernel that the plan counts on.  Its registers allow no more, but for heads of 64 with 32 and 48
@@ -113,11 +117,22 @@ constexpr bool tile_kernel_exists(int D, bool cache, int waves, bool tiny)
     return tiny ? !cache && waves == 4 : waves == 4 || (waves == 8 && (cache || D > 64));
 }
 
+// Attention over shared prefixes: the prefixes' part, the sequences' own part, and the workspace of all parts
+struct SharedPlan {
+    AttnPlan prefix, own;
+    int64_t workspace;
+};
+SharedPlan plan_shared_attention(int prefixes, int64_t max_sharing, int64_t max_prefix, int batch, int heads, int group, int D, int64_t tokens, int max_queries,
+                                 int64_t max_length);
+
 // SHFLBW_OK, or why the cache cannot be used (host checks of its fields)
 int check_cache(const shflbw_kv_cache* cache);
 // The launchers of attention_kernel.hip, one translation unit per operand format: the kernel that the plan says, and the join of
 // its parts.  prompt: keys and values in a.k and a.v.
 int run_attention_f16(const AttnArgs& a, const AttnPlan& plan, int head_dim, bool prompt, void* stream);
 int run_attention_bf16(const AttnArgs& a, const AttnPlan& plan, int head_dim, bool prompt, void* stream);
+// The same for both parts of attention over shared prefixes, whose parts lie one behind the other, and the join of all
+int run_shared_attention_f16(const AttnArgs& prefix, const AttnArgs& own, const SharedPlan& plan, int head_dim, void* stream);
+int run_shared_attention_bf16(const AttnArgs& prefix, const AttnArgs& own, const SharedPlan& plan, int head_dim, void* stream);
 
 }  // namespace shflbw

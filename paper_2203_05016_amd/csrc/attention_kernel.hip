@@ -126,7 +126,16 @@ __device__ __forceinline__ AttnSeq attn_sequence(const AttnArgs& a, int b)
 {
     AttnSeq s;
     int64_t t0 = CACHE ? b : 0, t1 = CACHE ? b + 1 : a.tokens;
-    if (a.starts) {
+    if (CACHE && a.shared) {
+        t0 = a.members ? attn_scalar(a.members)[b] : 0;
+        t1 = a.members ? attn_scalar(a.members)[b + 1] : a.sequences;
+        t0 = t0 < 0 ? 0 : t0 > a.sequences ? a.sequences : t0;
+        t1 = t1 < t0 ? t0 : t1 > a.sequences ? a.sequences : t1;
+        if (a.starts) {
+            t0 = attn_scalar(a.starts)[t0];
+            t1 = attn_scalar(a.starts)[t1];
+        }
+    } else if (a.starts) {
         t0 = attn_scalar(a.starts)[b];
         t1 = attn_scalar(a.starts)[b + 1];
     }
@@ -221,7 +230,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
     if (left <= 0) return;
     const int cols = (left < C / a.group ? left : C / a.group) * a.group;
     seq.t0 += skipped;
-    const int p_first = seq.len - left, p_last = p_first + (cols - 1) / a.group;
+    const int p_first = a.shared ? seq.len - 1 : seq.len - left, p_last = a.shared ? p_first : p_first + (cols - 1) / a.group;
     const AttnTiles tiles = attn_tiles(p_first, p_last, a.window, a.sinks, 0, ATTN_DECODE_KEYS);
     const int v_begin = split * a.split_tiles;
     // the last part takes what is left, also of a sequence longer than the plan was told
@@ -298,7 +307,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
 #pragma unroll
             for (int k = 0; k < D / (W * FS); ++k) *reinterpret_cast<uint16_t*>(smem + c * QP + (f0 + k * W * FS) * 2) = real ? x[k] : 0;
         // where a column's results go: head and token
-        if (wave == 0 && n < C) where[c] = a.splits == 1 ? (int64_t)(h * a.group + g) * D * a.ldo + seq.t0 + i
+        if (wave == 0 && n < C) where[c] = !a.part_o ? (int64_t)(h * a.group + g) * D * a.ldo + seq.t0 + i
                                                          : ((int64_t)split * a.heads * a.group + h * a.group + g) * a.tokens + seq.t0 + i;
         __syncthreads();
 #pragma unroll
@@ -309,7 +318,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int col = 16 * n + r;
-            p[n] = col < cols ? p_first + col / a.group : -1;
+            p[n] = col < cols ? p_first + (a.shared ? 0 : col / a.group) : -1;
             lo[n] = attn_window_start(p[n], a.window);
         }
     }
@@ -456,9 +465,9 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
         for (int i = 0; i < W; ++i) total += stat[i][col][1] * attn_exp2(stat[i][col][0] - top);
         if (seq.bad) total = __builtin_nanf("");
         float f = attn_exp2(m[n] - top);
-        if (a.splits == 1) f = p[n] < 0 ? 0 : f / total;
+        if (!a.part_o) f = p[n] < 0 ? 0 : f / total;
         else if (seq.bad) f = total;
-        if (a.splits > 1 && wave == 0 && quarter == 0 && col < cols) {
+        if (a.part_o && wave == 0 && quarter == 0 && col < cols) {
             const int64_t row = where[col];
             a.part_ml[2 * row] = p[n] < 0 ? -INFINITY : top;
             a.part_ml[2 * row + 1] = total;
@@ -473,7 +482,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
             float x = 0;
 #pragma unroll
             for (int i = 0; i < W; ++i) x += sums[(i * 16 + c) * OP + d];
-            if (a.splits == 1) a.out[where[at] + d * a.ldo] = attn_narrow<BF>(x);
+            if (!a.part_o) a.out[where[at] + d * a.ldo] = attn_narrow<BF>(x);
             else a.part_o[where[at] * D + d] = x;
         }
         __syncthreads();
@@ -612,7 +621,7 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
     const int64_t item_last = items < item0 + W ? items - 1 : item0 + W - 1;
     const int shift = CACHE ? 0 : (int)(seq.t0 & 7);       // tiles of a prompt begin at multiples of 8 columns
     const int p0 = seq.len - seq.nq;
-    const auto position = [&](int64_t query) { return p0 + (int)(query < seq.nq ? query : seq.nq - 1); };
+    const auto position = [&](int64_t query) { return CACHE && a.shared ? seq.len - 1 : p0 + (int)(query < seq.nq ? query : seq.nq - 1); };
     const int wg_first = position(item0 / a.group * ATTN_TILE_QUERIES);
     const int wg_last = position(item_last / a.group * ATTN_TILE_QUERIES + ATTN_TILE_QUERIES - 1);
     const AttnTiles tiles = attn_tiles(wg_first, wg_last, a.window, a.sinks, shift, ATTN_TILE_KEYS);
@@ -982,7 +991,7 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
     if (!works || query >= seq.nq) return;
     if (seq.bad) l = __builtin_nanf("");
     const int64_t token = seq.t0 + query;
-    if (a.splits == 1) {
+    if (!a.part_o) {
         const float f = p < 0 ? 0 : 1 / l;
         uint16_t* dst = a.out + ((int64_t)head * D + 4 * half) * a.ldo + token;
 #pragma unroll
@@ -1015,22 +1024,27 @@ __global__ __launch_bounds__(FEW ? 256 : 1024) void attention_join_kernel(AttnAr
     __shared__ float tile[FEW ? 4 : TOKENS][D + 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t token0 = (int64_t)blockIdx.x * TOKENS;
+    int64_t begin = 0, end = a.tokens;
+    if (a.shared && a.starts) {                            // columns of no sequence have no parts
+        begin = a.starts[0];
+        end = a.starts[a.sequences] < end ? a.starts[a.sequences] : end;
+    }
     const int head = blockIdx.y;
     const int64_t stride = (int64_t)a.heads * a.group * a.tokens;
     const bool has = 2 * lane < D;
     const int c = FEW ? 0 : wave;
-    if (token0 + c < a.tokens) {
+    if (token0 + c >= begin && token0 + c < end) {
         const int64_t at = (int64_t)head * a.tokens + token0 + c;
-        float top = -FLT_MAX, total = 0;
+        float top = -INFINITY, total = 0;
         for (int i = 0; i < a.splits; i += 64) {
             const int part = i + lane;
-            const float m = part < a.splits ? a.part_ml[2 * (at + part * stride)] : -FLT_MAX;
+            const float m = part < a.splits ? a.part_ml[2 * (at + part * stride)] : -INFINITY;
             top = fmaxf(top, m);
         }
 #pragma unroll
         for (int by = 1; by < 64; by *= 2) top = fmaxf(top, __shfl_xor(top, by));
         float2v x = {0, 0};
-        const bool none = a.part_ml[2 * at] == -INFINITY;
+        const bool none = top == -INFINITY;                // no part sees a key
 #pragma unroll 8
         for (int i = FEW ? wave : 0; i < a.splits; i += FEW ? 4 : 1) {
             const float f = attn_exp2(a.part_ml[2 * (at + i * stride)] - top);
@@ -1061,7 +1075,7 @@ __global__ __launch_bounds__(FEW ? 256 : 1024) void attention_join_kernel(AttnAr
 #pragma unroll
         for (int e = threadIdx.x; e < TOKENS * D; e += 1024) {
             const int c = e & 15, d = e >> 4;
-            if (token0 + c < a.tokens) a.out[((int64_t)head * D + d) * a.ldo + token0 + c] = attn_narrow<BF>(tile[c][d]);
+            if (token0 + c >= begin && token0 + c < end) a.out[((int64_t)head * D + d) * a.ldo + token0 + c] = attn_narrow<BF>(tile[c][d]);
         }
     }
 }

@@ -83,6 +83,16 @@ AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t to
     return p;
 }
 
+SharedPlan plan_shared_attention(int prefixes, int64_t max_sharing, int64_t max_prefix, int batch, int heads, int group, int D, int64_t tokens, int max_queries,
+                                 int64_t max_length)
+{
+    SharedPlan p = {};
+    p.prefix = plan_cache_attention(prefixes, heads, group, D, tokens, (int)std::min<int64_t>(max_sharing, INT32_MAX), max_prefix, INT32_MAX, 0);
+    p.own = plan_cache_attention(batch, heads, group, D, tokens, max_queries, max_length, INT32_MAX, 0);
+    p.workspace = product((int64_t)(p.prefix.splits + p.own.splits) * (D + 2) * 4, (int64_t)heads * group * tokens);
+    return p;
+}
+
 AttnPlan plan_prompt(int sequences, int heads, int group, int D, int64_t max_tokens, int window, int sinks, int64_t tokens)
 {
     AttnPlan p = {};
