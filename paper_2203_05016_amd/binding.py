@@ -180,6 +180,8 @@ def _load_calls():
               torch._C._cuda_getCurrentRawStream)
     m.connect_attention(address(L.shflbw_kv_write), address(L.shflbw_kv_read), address(L.shflbw_kv_attention_workspace),
                         address(L.shflbw_kv_attention), address(L.shflbw_window_attention))
+    m.connect_serving(address(L.shflbw_norm_rotate), address(L.shflbw_kv_shared_attention_workspace), address(L.shflbw_kv_shared_attention),
+                      address(L.shflbw_kv_pages_workspace), address(L.shflbw_kv_extend), address(L.shflbw_kv_fork), address(L.shflbw_kv_compact))
     return m
 
 
@@ -645,6 +647,13 @@ class KVCache:
         ``members[g + 1] - 1``; without members one prefix is everybody's.  max_prefix: the longest prefix's tokens (all of the table's pages by
         default), which decides how the work is cut only.  max_sharing: at least the columns of q that any prefix's sequences have
         together (all of them by default)."""
+        if stream is None and self._plan is not None:
+            r = _calls.shared_attention(self._plan, q, prefix_table, prefix_lengths, table, lengths, members, starts, max_queries, max_length, max_prefix,
+                                        max_sharing, out)   # None: not the plain case, all checks below
+            if r is not None:
+                if type(r) is int:
+                    _check(r)
+                return r if out is None else out
         import torch
         if q.dtype != self.dtype or q.dim() != 2 or q.shape[0] == 0 or q.shape[0] % (self.heads * self.head_dim):
             raise TypeError("q must be a 2-D %s tensor with a multiple of %d rows" % (self.dtype, self.heads * self.head_dim))
@@ -718,6 +727,12 @@ class KVCache:
         int32 how many entries of tables name each page; counts (sequences,) int32.  tokens: how many slots are wanted, at least what
         counts add up to.  Returns (table, lengths, uses, slots, starts): slots (tokens,) for ``write``, -1 where there is no page left and past the last token,
         starts (sequences + 1,) for ``attention``.  out: the first three's memory, which may be the arguments' own; slots, starts: theirs."""
+        if stream is None and self._plan is not None:
+            r = _calls.kv_extend(self._plan, table, lengths, uses, counts, tokens, out, slots, starts)   # None: not the plain case
+            if r is not None:
+                if type(r) is int:
+                    _check(r)
+                return r
         import torch
         _natural(tokens=tokens)
         rows = table.shape[0] if table.dim() else 0
@@ -741,6 +756,12 @@ class KVCache:
         Full pages are shared; a last page that is not full is copied to a free one for all but the first that continues its
         row.  Rows that nothing continues give their pages up.  Returns the new (table, lengths, uses); out: their memory, which
         must not be the arguments' own but for uses."""
+        if stream is None and self._plan is not None:
+            r = _calls.kv_fork(self._plan, table, lengths, uses, parents, out)   # None: not the plain case
+            if r is not None:
+                if type(r) is int:
+                    _check(r)
+                return r
         rows = parents.shape[0] if parents.dim() else 0
         _indices(parents, "parents", rows)
         before, after, out = self._held("fork", table, lengths, uses, out, rows, stream)
@@ -755,6 +776,12 @@ class KVCache:
         """Moves the pages in use to the front of the cache, as few of them as possible: with n in use they are pages 0 to n - 1 afterwards.
 
         Returns the new (table, uses); out: their memory, which may be the arguments' own.  Every table in use has to be part of this one."""
+        if stream is None and self._plan is not None:
+            r = _calls.kv_compact(self._plan, table, uses, out)   # None: not the plain case
+            if r is not None:
+                if type(r) is int:
+                    _check(r)
+                return r
         rows = table.shape[0] if table.dim() else 0
         before, after, out = self._held("compact", table, None, uses, out, rows, stream)
         on, handle = _launch_on(self.device, stream)
@@ -772,6 +799,12 @@ def norm_rotate(q, k, head_dim, positions, frequencies, axes=None, q_weight=None
     frequencies (pairs,) float64: radians per step of the position for each pair of features, i and i + pairs (interleaved: 2 i and 2 i + 1); the
     features past 2 * pairs are not turned.  positions (tokens,) or (rows, tokens) int32; axes (pairs,) int32: which row each pair goes by, the first
     without it.  All on the GPU.  Returns (q, k) of q's dtype; q_out, k_out: their memory, which may be q and k themselves."""
+    if stream is None and (_calls or calls()):
+        r = _calls.norm_rotate(q, k, head_dim, positions, frequencies, axes, q_weight, k_weight, eps, norm, interleaved, q_out, k_out)
+        if r is not None:                       # None: not the plain case, all checks below
+            if type(r) is int:
+                _check(r)
+            return r
     import torch
     if q.dtype not in (torch.float16, torch.bfloat16) or q.dim() != 2:
         raise TypeError("q must be a 2-D float16 or bfloat16 tensor")

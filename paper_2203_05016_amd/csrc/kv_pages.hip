@@ -19,6 +19,10 @@ namespace {
 constexpr int PAGES_BLOCK = 4096;          // pages to a workgroup of 1024 threads
 constexpr int COPY_BYTES = 16384;          // bytes of a page to a workgroup of 256 threads
 constexpr int MOST_BLOCKS = 16384;         // of a launch whose workgroups take pieces in turn
+constexpr int FEW_PAGES = 16384;           // of a cache whose books one workgroup keeps
+constexpr int FEW_ROWS = 2048;
+constexpr int64_t FEW_ENTRIES = 32768;     // entries, and slots, that it works out
+static_assert(PAGES_BLOCK == 4 * 1024, "rank_flags takes four runs of 1024");
 
 typedef unsigned copy4 __attribute__((ext_vector_type(4)));
 
@@ -53,27 +57,76 @@ __device__ __forceinline__ int open_entry(const PagesArgs& a, int length)
     return j < a.width ? j : -1;
 }
 
-// the sum of x over the threads before this one, and over all 1024 of them
+// ---- sums over a workgroup of 1024 threads
+//
+// A wavefront's running sum by moves between lanes' registers; `shared` is 64 numbers of LDS that nothing else uses.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved_lanes(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, true); }
+__device__ __forceinline__ int wave_sum(int x)               // over this lane and those before it
+{
+    x += moved_lanes<0x111, 0xf>(x);                         // by 1, 2, 4, 8 in rows of 16
+    x += moved_lanes<0x112, 0xf>(x);
+    x += moved_lanes<0x114, 0xf>(x);
+    x += moved_lanes<0x118, 0xf>(x);
+    x += moved_lanes<0x142, 0xa>(x);                         // the last of row 0 to 1, of 2 to 3
+    x += moved_lanes<0x143, 0xc>(x);                         // the last of 1 to 2 and 3
+    return x;
+}
+__device__ __forceinline__ int64_t wave_sum64(int64_t x)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int by = 1; by < 64; by *= 2) {
+        const int64_t y = __shfl_up(x, by);
+        if (lane >= by) x += y;
+    }
+    return x;
+}
+// the sum of x over the threads before this one, and over all
 struct Scan {
     int64_t before, all;
 };
 __device__ __forceinline__ Scan scan_block(int64_t x, int64_t* shared)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t sum = x;
-#pragma unroll
-    for (int by = 1; by < 64; by *= 2) {
-        const int64_t y = __shfl_up(sum, by);
-        if (lane >= by) sum += y;
-    }
+    const int64_t sum = wave_sum64(x);
     if (lane == 63) shared[wave] = sum;
     __syncthreads();
-    Scan r = {sum - x, 0};
+    const int64_t mine = lane < 16 ? shared[lane] : 0, waves = wave_sum64(mine);
+    const Scan r = {__shfl(waves - mine, wave) + sum - x, __shfl(waves, 15)};
+    __syncthreads();
+    return r;
+}
+__device__ __forceinline__ int sum_block(int x, int64_t* shared)
+{
+    int* counts = reinterpret_cast<int*>(shared);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sum = wave_sum(x);
+    if (lane == 63) counts[wave] = sum;
+    __syncthreads();
+    const int all = __builtin_amdgcn_readlane(wave_sum(lane < 16 ? counts[lane] : 0), 63);
+    __syncthreads();
+    return all;
+}
+// Four runs of 1024 flags, a thread's at its own number in each: how many are set before each of the thread's, and in all.
+struct Ranks {
+    int before[4], all;
+};
+__device__ __forceinline__ Ranks rank_flags(const bool (&flag)[4], int64_t* shared)
+{
+    int* counts = reinterpret_cast<int*>(shared);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Ranks r;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) {
-        if (w < wave) r.before += shared[w];
-        r.all += shared[w];
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t set = __ballot(flag[i]);
+        r.before[i] = (int)__builtin_amdgcn_mbcnt_hi((unsigned)(set >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)set, 0));
+        if (lane == 0) counts[i * 16 + wave] = __popcll(set);
     }
+    __syncthreads();
+    const int mine = counts[lane], sum = wave_sum(mine);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.before[i] += __builtin_amdgcn_readlane(sum - mine, i * 16 + wave);
+    r.all = __builtin_amdgcn_readlane(sum, 63);
     __syncthreads();
     return r;
 }
@@ -88,48 +141,88 @@ __device__ __forceinline__ void count_pages(const PagesArgs& a, const int32_t* u
     int n = 0;
 #pragma unroll
     for (int i = 0; i < PAGES_BLOCK / 1024; ++i) n += counted<LIVE_PAGES>(uses, block * PAGES_BLOCK + i * 1024 + threadIdx.x, a.pages);
-    const Scan s = scan_block(n, shared);
-    if (threadIdx.x == 0) a.counts[block] = (int)s.all;
+    n = sum_block(n, shared);
+    if (threadIdx.x == 0) a.counts[block] = n;
 }
-// calls f(page, whether it is counted, how many are before it) for every page of the block; returns how many there are in all
+// Calls f(page, whether it is counted, how many are before it) for every page of the block, of which `before` are in earlier ones; returns how many are up to
+// its end.  A page is looked at before f may change its count.
 template <bool LIVE_PAGES, class F>
-__device__ __forceinline__ int rank_pages(const PagesArgs& a, const int32_t* uses, int block, int64_t* shared, F&& f)
+__device__ __forceinline__ int rank_block(const PagesArgs& a, const int32_t* uses, int block, int before, int64_t* shared, F&& f)
 {
-    int64_t mine = 0, rest = 0;
-    for (int i = threadIdx.x; i < a.page_blocks; i += 1024) (i < block ? mine : rest) += a.counts[i];
-    int before = (int)scan_block(mine, shared).all;
-    const int total = before + (int)scan_block(rest, shared).all;
-    // (both in one pass over the block: a page is looked at before f may change its count)
-    bool is[PAGES_BLOCK / 1024];
+    bool is[4];
 #pragma unroll
-    for (int i = 0; i < PAGES_BLOCK / 1024; ++i) is[i] = counted<LIVE_PAGES>(uses, block * PAGES_BLOCK + i * 1024 + threadIdx.x, a.pages);
+    for (int i = 0; i < 4; ++i) is[i] = counted<LIVE_PAGES>(uses, block * PAGES_BLOCK + i * 1024 + threadIdx.x, a.pages);
+    const Ranks r = rank_flags(is, shared);
 #pragma unroll
-    for (int i = 0; i < PAGES_BLOCK / 1024; ++i) {
-        const Scan s = scan_block(is[i], shared);
-        f(block * PAGES_BLOCK + i * 1024 + (int)threadIdx.x, is[i], before + (int)s.before, total);
-        before += (int)s.all;
+    for (int i = 0; i < 4; ++i) f(block * PAGES_BLOCK + i * 1024 + (int)threadIdx.x, is[i], before + r.before[i]);
+    return before + r.all;
+}
+// The counts of up to FEW_PAGES pages in registers of one workgroup, all brought at once; rank_few as rank_block over them, f being given the count too
+struct FewUses {
+    int of[FEW_PAGES / 1024];
+};
+__device__ __forceinline__ FewUses load_few(const PagesArgs& a)
+{
+    FewUses u;
+#pragma unroll
+    for (int i = 0; i < FEW_PAGES / 1024; ++i) {
+        const int p = i * 1024 + (int)threadIdx.x;
+        u.of[i] = a.uses_in[p < a.pages ? p : a.pages - 1];
     }
-    return total;
+    return u;
+}
+template <bool LIVE_PAGES, class F>
+__device__ __forceinline__ int rank_few(const PagesArgs& a, const FewUses& u, int64_t* shared, F&& f)
+{
+    int before = 0;
+#pragma unroll
+    for (int b = 0; b < FEW_PAGES / PAGES_BLOCK; ++b) {
+        if (b >= a.page_blocks) break;
+        bool is[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) is[i] = b * PAGES_BLOCK + i * 1024 + (int)threadIdx.x < a.pages && (LIVE_PAGES ? u.of[4 * b + i] != 0 : u.of[4 * b + i] == 0);
+        const Ranks r = rank_flags(is, shared);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f(b * PAGES_BLOCK + i * 1024 + (int)threadIdx.x, is[i], before + r.before[i], u.of[4 * b + i]);
+        before += r.all;
+    }
+    return before;
+}
+// what is counted in the blocks before, and in all: of counts that count_pages left
+struct Counted {
+    int before, all;
+};
+__device__ __forceinline__ Counted counted_blocks(const PagesArgs& a, int block, int64_t* shared)
+{
+    int mine = 0, rest = 0;
+    for (int i = threadIdx.x; i < a.page_blocks; i += 1024) (i < block ? mine : rest) += a.counts[i];
+    const int before = sum_block(mine, shared);
+    return Counted{before, before + sum_block(rest, shared)};
 }
 
-// the lowest totals[WANTED] free pages, in order; they are in use from here on
+// the lowest `wanted` free pages, in order; they are in use from here on
+__device__ __forceinline__ void take_page(const PagesArgs& a, int32_t* list, int wanted, int p, bool free, int rank, int uses)
+{
+    if (p >= a.pages) return;
+    const bool taken = free && rank < wanted;
+    if (taken) list[rank] = p;
+    a.uses_out[p] = taken ? 1 : uses;
+}
 __global__ __launch_bounds__(1024) void pages_take_kernel(PagesArgs a, const int32_t* uses)
 {
-    __shared__ int64_t shared[16];
+    __shared__ int64_t shared[64];
+    const Counted n = counted_blocks(a, blockIdx.x, shared);
     const int wanted = a.totals[WANTED];
-    const int total = rank_pages<false>(a, uses, blockIdx.x, shared, [&](int p, bool free, int rank, int) {
-        if (p >= a.pages) return;
-        const bool taken = free && rank < wanted;
-        if (taken) a.list[rank] = p;
-        a.uses_out[p] = taken ? 1 : uses[p];
+    rank_block<false>(a, uses, blockIdx.x, n.before, shared, [&](int p, bool free, int rank) {
+        if (p < a.pages) take_page(a, a.list, wanted, p, free, rank, uses[p]);
     });
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.totals[FREE] = total;
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.totals[FREE] = n.all;
 }
 // the page of rank `rank` among those taken, or -1
-__device__ __forceinline__ int taken_page(const PagesArgs& a, int64_t rank) { return rank < a.totals[FREE] ? a.list[rank] : -1; }
+__device__ __forceinline__ int taken_page(const PagesArgs& a, int64_t rank, int free) { return rank < free ? a.list[rank] : -1; }
 
 // ---- more tokens
-__device__ __forceinline__ void extend_rows(const PagesArgs& a, int64_t* shared)
+__device__ __forceinline__ int64_t extend_rows(const PagesArgs& a, int64_t* shared)   // returns the pages that are wanted
 {
     int64_t pages = 0, tokens = 0;
     for (int b0 = 0; b0 < a.rows; b0 += 1024) {
@@ -152,46 +245,64 @@ __device__ __forceinline__ void extend_rows(const PagesArgs& a, int64_t* shared)
         pages += p.all;
         tokens += t.all;
     }
-    if (threadIdx.x == 0) {
-        a.starts[a.rows] = tokens < INT_MAX ? (int)tokens : INT_MAX;
-        a.totals[WANTED] = pages < INT_MAX ? (int)pages : INT_MAX;
+    if (threadIdx.x == 0) a.starts[a.rows] = tokens < INT_MAX ? (int)tokens : INT_MAX;
+    return pages;
+}
+// A row's entries and its tokens' slots, by `step` threads of which this is `first`.  Row a.rows is that of the slots past the last token.
+__device__ __forceinline__ void extend_row(const PagesArgs& a, int b, int free, int first, int step)
+{
+    if (b == a.rows) {
+        for (int64_t t = (int64_t)a.starts[b] + first; t < a.tokens; t += step) a.slots[t] = -1;
+        return;
+    }
+    const int length = a.old_length[b], old = held(a, length), now = held(a, a.lengths_out[b]);
+    const int64_t base = (int64_t)a.base[b] - old;
+    const int32_t* in = a.table_in + b * a.ld_in;
+    int32_t* out = a.table_out + b * a.ld_out;
+    const auto entry = [&](int j) __attribute__((always_inline)) { return j < old ? in[j] : taken_page(a, base + j, free); };
+    for (int j = first; j < a.width; j += step) out[j] = j < now ? entry(j) : -1;
+    const int64_t start = a.starts[b], end = a.starts[b + 1] < a.tokens ? a.starts[b + 1] : a.tokens;
+    for (int64_t t = start + first; t < end; t += step) {
+        const int64_t at = length + (t - start), j = at >> a.page_shift;
+        const int page = j < a.width ? entry((int)j) : -1;
+        a.slots[t] = in_cache(a, page) ? (page << a.page_shift) + (int)(at & ((1 << a.page_shift) - 1)) : -1;
     }
 }
 __global__ __launch_bounds__(1024) void extend_count_kernel(PagesArgs a)
 {
-    __shared__ int64_t shared[16];
+    __shared__ int64_t shared[64];
     if ((int)blockIdx.x < a.page_blocks) count_pages<false>(a, a.uses_in, blockIdx.x, shared);
-    else extend_rows(a, shared);
-}
-// entry j of a sequence that had `old` of them
-__device__ __forceinline__ int extended(const PagesArgs& a, int b, int j, int old)
-{
-    return j < old ? a.table_in[b * a.ld_in + j] : taken_page(a, (int64_t)a.base[b] + j - old);
-}
-__global__ __launch_bounds__(256) void extend_apply_kernel(PagesArgs a)
-{
-    const int64_t entries = (int64_t)a.rows * a.width, step = (int64_t)gridDim.x * 256;
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < entries + a.tokens; e += step) {
-        if (e < entries) {
-            const int b = (int)(e / a.width), j = (int)(e % a.width), old = held(a, a.old_length[b]);
-            a.table_out[b * a.ld_out + j] = j < held(a, a.lengths_out[b]) ? extended(a, b, j, old) : -1;
-            continue;
-        }
-        const int64_t t = e - entries;
-        int slot = -1;
-        if (t < a.starts[a.rows]) {
-            int low = 0, high = a.rows;                    // starts[low] <= t < starts[high]
-            while (high - low > 1) {
-                const int mid = low + (high - low) / 2;
-                if (a.starts[mid] <= t) low = mid;
-                else high = mid;
-            }
-            const int64_t at = a.old_length[low] + t - a.starts[low], j = at >> a.page_shift;
-            const int page = j < a.width ? extended(a, low, (int)j, held(a, a.old_length[low])) : -1;
-            if (in_cache(a, page)) slot = (page << a.page_shift) + (int)(at & ((1 << a.page_shift) - 1));
-        }
-        a.slots[t] = slot;
+    else {
+        const int64_t pages = extend_rows(a, shared);
+        if (threadIdx.x == 0) a.totals[WANTED] = pages < INT_MAX ? (int)pages : INT_MAX;
     }
+}
+__global__ __launch_bounds__(256) void extend_apply_kernel(PagesArgs a, int parts)
+{
+    for (int64_t n = blockIdx.x; n < ((int64_t)a.rows + 1) * parts; n += gridDim.x)
+        extend_row(a, (int)(n / parts), a.totals[FREE], (int)(n % parts) * 256 + threadIdx.x, parts * 256);
+}
+// All of it by one workgroup: what the steps tell each other stays in the LDS.
+__global__ __launch_bounds__(1024) void extend_few_kernel(PagesArgs a)
+{
+    __shared__ int64_t shared[64];
+    __shared__ int32_t list[FEW_PAGES], base[FEW_ROWS], old_length[FEW_ROWS], length[FEW_ROWS], starts[FEW_ROWS + 1];
+    const FewUses uses = load_few(a);
+    PagesArgs b = a;
+    b.list = list;
+    b.base = base;
+    b.old_length = old_length;
+    b.lengths_out = length;
+    b.starts = starts;
+    const int64_t pages = extend_rows(b, shared);
+    const int wanted = pages < INT_MAX ? (int)pages : INT_MAX;
+    const int free = rank_few<false>(a, uses, shared, [&](int p, bool is_free, int rank, int n) { take_page(a, list, wanted, p, is_free, rank, n); });
+    __syncthreads();
+    for (int i = threadIdx.x; i <= a.rows; i += 1024) {
+        if (i < a.rows) a.lengths_out[i] = length[i];
+        a.starts[i] = starts[i];
+    }
+    for (int row = threadIdx.x >> 6; row <= a.rows; row += 16) extend_row(b, row, free, threadIdx.x & 63, 64);
 }
 
 // ---- sequences that continue others
@@ -199,42 +310,79 @@ __global__ __launch_bounds__(256) void extend_apply_kernel(PagesArgs a)
 // A row's children and the lowest of them; what every child wants of fresh pages (its open page, where it is not the lowest).
 __device__ __forceinline__ int load_shared(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ bool has_parent(const PagesArgs& a, int parent) { return (unsigned)parent < (unsigned)a.rows_in; }
-__global__ __launch_bounds__(1024) void fork_count_kernel(PagesArgs a)
+__device__ __forceinline__ void fork_children(const PagesArgs& a, int* first, int* children)   // of one workgroup, in the LDS
 {
-    __shared__ int64_t shared[16];
-    if (blockIdx.x) {                                      // the counts, to be changed
-        for (int64_t p = (int64_t)(blockIdx.x - 1) * 1024 + threadIdx.x; p < a.pages; p += (int64_t)(gridDim.x - 1) * 1024) a.uses_out[p] = a.uses_in[p];
-        return;
-    }
     for (int b = threadIdx.x; b < a.rows_in; b += 1024) {
-        __hip_atomic_store(a.first + b, INT_MAX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(a.children + b, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        first[b] = INT_MAX;
+        children[b] = 0;
     }
-    __threadfence();
     __syncthreads();
     for (int i = threadIdx.x; i < a.rows; i += 1024) {
         const int parent = a.which[i];
         if (!has_parent(a, parent)) continue;
-        atomicMin(a.first + parent, i);
-        atomicAdd(a.children + parent, 1);
+        atomicMin(first + parent, i);
+        atomicAdd(children + parent, 1);
     }
-    __threadfence();
     __syncthreads();
-    int64_t pages = 0;
-    for (int i0 = 0; i0 < a.rows; i0 += 1024) {
-        const int i = i0 + threadIdx.x;
-        bool need = false;
-        if (i < a.rows) {
+}
+// the new lengths, and what every child wants: its rank among those that want a page, or -1.  Returns how many do.
+template <class First>
+__device__ __forceinline__ int fork_wants(const PagesArgs& a, First&& first, int64_t* shared)
+{
+    int wanted = 0;
+    for (int i0 = 0; i0 < a.rows; i0 += 4096) {
+        bool need[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = i0 + k * 1024 + (int)threadIdx.x;
+            need[k] = false;
+            if (i >= a.rows) continue;
             const int parent = a.which[i];
             const int length = has_parent(a, parent) && a.lengths_in[parent] > 0 ? a.lengths_in[parent] : 0, j = open_entry(a, length);
             a.lengths_out[i] = length;
-            need = j >= 0 && load_shared(a.first + parent) != i && in_cache(a, a.table_in[parent * a.ld_in + j]);
+            need[k] = j >= 0 && first(parent) != i && in_cache(a, a.table_in[parent * a.ld_in + j]);
         }
-        const Scan s = scan_block(need, shared);
-        if (i < a.rows) a.base[i] = need ? (int)(pages + s.before) : -1;
-        pages += s.all;
+        const Ranks r = rank_flags(need, shared);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = i0 + k * 1024 + (int)threadIdx.x;
+            if (i < a.rows) a.base[i] = need[k] ? wanted + r.before[k] : -1;
+        }
+        wanted += r.all;
     }
-    if (threadIdx.x == 0) a.totals[WANTED] = (int)pages;
+    return wanted;
+}
+__global__ __launch_bounds__(1024) void fork_count_kernel(PagesArgs a)
+{
+    __shared__ int64_t shared[64];
+    __shared__ int first[FEW_ROWS], children[FEW_ROWS];
+    if (blockIdx.x) {                                      // the counts, to be changed
+        for (int64_t p = (int64_t)(blockIdx.x - 1) * 1024 + threadIdx.x; p < a.pages; p += (int64_t)(gridDim.x - 1) * 1024) a.uses_out[p] = a.uses_in[p];
+        return;
+    }
+    int wanted;
+    if (a.rows_in <= FEW_ROWS) {
+        fork_children(a, first, children);
+        for (int b = threadIdx.x; b < a.rows_in; b += 1024) a.children[b] = children[b];
+        wanted = fork_wants(a, [&](int b) __attribute__((always_inline)) { return first[b]; }, shared);
+    } else {
+        for (int b = threadIdx.x; b < a.rows_in; b += 1024) {
+            __hip_atomic_store(a.first + b, INT_MAX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(a.children + b, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __threadfence();
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.rows; i += 1024) {
+            const int parent = a.which[i];
+            if (!has_parent(a, parent)) continue;
+            atomicMin(a.first + parent, i);
+            atomicAdd(a.children + parent, 1);
+        }
+        __threadfence();
+        __syncthreads();
+        wanted = fork_wants(a, [&](int b) __attribute__((always_inline)) { return load_shared(a.first + b); }, shared);
+    }
+    if (threadIdx.x == 0) a.totals[WANTED] = wanted;
 }
 // Every old entry's page is named by as many entries as its row has children, an open one by the lowest's: the count changes by that less one.
 __global__ __launch_bounds__(256) void fork_table_kernel(PagesArgs a)
@@ -256,7 +404,7 @@ __global__ __launch_bounds__(256) void fork_table_kernel(PagesArgs a)
 }
 __global__ __launch_bounds__(1024) void pages_count_kernel(PagesArgs a)
 {
-    __shared__ int64_t shared[16];
+    __shared__ int64_t shared[64];
     count_pages<false>(a, a.uses_out, blockIdx.x, shared);
 }
 // piece `part` of page `from` to page `to`
@@ -282,10 +430,39 @@ __global__ __launch_bounds__(256) void fork_copy_kernel(PagesArgs a, int parts)
     for (int64_t n = blockIdx.x; n < (int64_t)a.rows * parts; n += gridDim.x) {
         const int i = (int)(n / parts), part = (int)(n % parts), rank = a.base[i];
         if (rank < 0) continue;
-        const int parent = a.which[i], j = open_entry(a, a.lengths_in[parent]), to = taken_page(a, rank);
+        const int parent = a.which[i], j = open_entry(a, a.lengths_in[parent]), to = taken_page(a, rank, a.totals[FREE]);
         if (part == 0 && threadIdx.x == 0) a.table_out[i * a.ld_out + j] = to;
         if (to >= 0) copy_piece(a, a.table_in[parent * a.ld_in + j], to, part);
     }
+}
+
+// All but the copies by one workgroup, with the counts and the rows' children in the LDS.
+__global__ __launch_bounds__(1024) void fork_few_kernel(PagesArgs a)
+{
+    __shared__ int64_t shared[64];
+    __shared__ int uses[FEW_PAGES], first[FEW_ROWS], children[FEW_ROWS];
+    for (int p = threadIdx.x; p < a.pages; p += 1024) uses[p] = a.uses_in[p];
+    fork_children(a, first, children);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int b = wave; b < a.rows_in; b += 16) {           // (as fork_table_kernel)
+        const int length = a.lengths_in[b], n = held(a, length), open = open_entry(a, length), named = children[b];
+        for (int j = lane; j < n; j += 64) {
+            const int page = a.table_in[b * a.ld_in + j], change = (j == open && named > 1 ? 1 : named) - 1;
+            if (change && in_cache(a, page)) atomicAdd(uses + page, change);
+        }
+    }
+    for (int i = wave; i < a.rows; i += 16) {
+        const int parent = a.which[i], n = has_parent(a, parent) ? held(a, a.lengths_in[parent]) : 0;
+        for (int j = lane; j < a.width; j += 64) a.table_out[i * a.ld_out + j] = j < n ? a.table_in[parent * a.ld_in + j] : -1;
+    }
+    const int wanted = fork_wants(a, [&](int b) __attribute__((always_inline)) { return first[b]; }, shared);
+    __syncthreads();
+    int free = 0;
+    for (int block = 0; block < a.page_blocks; ++block)
+        free = rank_block<false>(a, uses, block, free, shared, [&](int p, bool is_free, int rank) {
+            if (p < a.pages) take_page(a, a.list, wanted, p, is_free, rank, uses[p]);
+        });
+    if (threadIdx.x == 0) a.totals[FREE] = free;
 }
 
 // ---- pages in use to the front
@@ -293,31 +470,44 @@ __global__ __launch_bounds__(256) void fork_copy_kernel(PagesArgs a, int parts)
 // With n of them: those from n on have ranks totals[LIVE_BELOW] and up among the pages in use, and as many pages below n are free; the i-th goes to the i-th.
 __global__ __launch_bounds__(1024) void compact_count_kernel(PagesArgs a)
 {
-    __shared__ int64_t shared[16];
+    __shared__ int64_t shared[64];
     count_pages<true>(a, a.uses_in, blockIdx.x, shared);
+}
+__device__ __forceinline__ void place_page(const PagesArgs& a, int total, int p, bool live, int rank, int uses)   // of `total` pages in use
+{
+    if (p == total || (p == a.pages - 1 && total == a.pages)) {
+        a.totals[LIVE_BELOW] = p == total ? rank : total;
+        a.totals[LIVE] = total;
+    }
+    if (p >= a.pages) return;
+    if (p < total) {
+        if (live) a.uses_out[p] = uses;
+        else a.list[p - rank] = p;                         // (its count comes with the page that moves here)
+    } else {
+        a.rank[p] = live ? rank : -1;
+        a.uses_out[p] = 0;
+        if (live) {
+            a.source[rank] = p;
+            a.moved[rank] = uses;
+        }
+    }
 }
 __global__ __launch_bounds__(1024) void compact_rank_kernel(PagesArgs a)
 {
-    __shared__ int64_t shared[16];
-    rank_pages<true>(a, a.uses_in, blockIdx.x, shared, [&](int p, bool live, int rank, int total) {
-        if (p == total || (p == a.pages - 1 && total == a.pages)) {
-            a.totals[LIVE_BELOW] = p == total ? rank : total;
-            a.totals[LIVE] = total;
-        }
-        if (p >= a.pages) return;
-        const int uses = a.uses_in[p];
-        if (p < total) {
-            if (live) a.uses_out[p] = uses;
-            else a.list[p - rank] = p;                     // (its count comes with the page that moves here)
-        } else {
-            a.rank[p] = live ? rank : -1;
-            a.uses_out[p] = 0;
-            if (live) {
-                a.source[rank] = p;
-                a.moved[rank] = uses;
-            }
-        }
-    });
+    __shared__ int64_t shared[64];
+    const Counted n = counted_blocks(a, blockIdx.x, shared);
+    rank_block<true>(a, a.uses_in, blockIdx.x, n.before, shared, [&](int p, bool live, int rank) { place_page(a, n.all, p, live, rank, p < a.pages ? a.uses_in[p] : 0); });
+}
+// by one workgroup, without the counts of another launch
+__global__ __launch_bounds__(1024) void compact_few_kernel(PagesArgs a)
+{
+    __shared__ int64_t shared[64];
+    const FewUses uses = load_few(a);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < FEW_PAGES / 1024; ++i) n += i * 1024 + (int)threadIdx.x < a.pages && uses.of[i] != 0;
+    const int total = sum_block(n, shared);
+    rank_few<true>(a, uses, shared, [&](int p, bool live, int rank, int count) { place_page(a, total, p, live, rank, count); });
 }
 __global__ __launch_bounds__(256) void compact_apply_kernel(PagesArgs a, int parts, int table_blocks)
 {
@@ -455,9 +645,15 @@ int shflbw_kv_extend(const shflbw_kv_cache* cache, const shflbw_kv_pages* in, co
     a.starts = starts;
     a.tokens = tokens;
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (a.pages <= FEW_PAGES && a.rows <= FEW_ROWS && (int64_t)a.rows * a.width + tokens <= FEW_ENTRIES) {
+        hipLaunchKernelGGL(extend_few_kernel, dim3(1), dim3(1024), 0, st, a);
+        return launched();
+    }
     hipLaunchKernelGGL(extend_count_kernel, dim3(a.page_blocks + 1), dim3(1024), 0, st, a);
     hipLaunchKernelGGL(pages_take_kernel, dim3(a.page_blocks), dim3(1024), 0, st, a, a.uses_in);
-    hipLaunchKernelGGL(extend_apply_kernel, dim3(few_blocks(ceil_div((int64_t)a.rows * a.width + tokens, 256))), dim3(256), 0, st, a);
+    // workgroups to a row, for 1024 of its entries and slots each
+    const int parts = (int)few_blocks(ceil_div((int64_t)a.rows * a.width + tokens, ((int64_t)a.rows + 1) * 1024));
+    hipLaunchKernelGGL(extend_apply_kernel, dim3(few_blocks(((int64_t)a.rows + 1) * parts)), dim3(256), 0, st, a, parts);
     return launched();
 }
 
@@ -472,6 +668,11 @@ int shflbw_kv_fork(const shflbw_kv_cache* cache, const shflbw_kv_pages* in, cons
     a.which = parents;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int parts = (int)ceil_div(a.page_bytes, COPY_BYTES);
+    if (a.pages <= FEW_PAGES && a.rows_in <= FEW_ROWS && ((int64_t)a.rows_in + a.rows) * a.width <= FEW_ENTRIES) {
+        hipLaunchKernelGGL(fork_few_kernel, dim3(1), dim3(1024), 0, st, a);
+        hipLaunchKernelGGL(fork_copy_kernel, dim3(few_blocks((int64_t)a.rows * parts)), dim3(256), 0, st, a, parts);
+        return launched();
+    }
     hipLaunchKernelGGL(fork_count_kernel, dim3(a.uses_in == a.uses_out ? 1 : 1 + few_blocks(ceil_div(a.pages, 1024))), dim3(1024), 0, st, a);
     hipLaunchKernelGGL(fork_table_kernel, dim3(few_blocks(ceil_div(((int64_t)a.rows_in + a.rows) * a.width, 256))), dim3(256), 0, st, a);
     hipLaunchKernelGGL(pages_count_kernel, dim3(a.page_blocks), dim3(1024), 0, st, a);
@@ -491,8 +692,12 @@ int shflbw_kv_compact(const shflbw_kv_cache* cache, const shflbw_kv_pages* in, c
     const int parts = (int)ceil_div(a.page_bytes, COPY_BYTES), table_blocks = (int)few_blocks(ceil_div((int64_t)a.rows * a.width, 256));
     // at most half of the pages move
     const unsigned copy_blocks = few_blocks((int64_t)(a.pages / 2) * parts);
-    hipLaunchKernelGGL(compact_count_kernel, dim3(a.page_blocks), dim3(1024), 0, st, a);
-    hipLaunchKernelGGL(compact_rank_kernel, dim3(a.page_blocks), dim3(1024), 0, st, a);
+    if (a.pages <= FEW_PAGES) {
+        hipLaunchKernelGGL(compact_few_kernel, dim3(1), dim3(1024), 0, st, a);
+    } else {
+        hipLaunchKernelGGL(compact_count_kernel, dim3(a.page_blocks), dim3(1024), 0, st, a);
+        hipLaunchKernelGGL(compact_rank_kernel, dim3(a.page_blocks), dim3(1024), 0, st, a);
+    }
     hipLaunchKernelGGL(compact_apply_kernel, dim3(table_blocks + copy_blocks), dim3(256), 0, st, a, parts, table_blocks);
     return launched();
 }

@@ -33,6 +33,13 @@ typedef decltype(&shflbw_kv_read) kv_read_fn;
 typedef decltype(&shflbw_kv_attention_workspace) kv_workspace_fn;
 typedef decltype(&shflbw_kv_attention) kv_attention_fn;
 typedef decltype(&shflbw_window_attention) window_attention_fn;
+typedef decltype(&shflbw_norm_rotate) norm_rotate_fn;
+typedef decltype(&shflbw_kv_shared_attention_workspace) shared_workspace_fn;
+typedef decltype(&shflbw_kv_shared_attention) shared_attention_fn;
+typedef decltype(&shflbw_kv_pages_workspace) pages_workspace_fn;
+typedef decltype(&shflbw_kv_extend) kv_extend_fn;
+typedef decltype(&shflbw_kv_fork) kv_fork_fn;
+typedef decltype(&shflbw_kv_compact) kv_compact_fn;
 
 spmm_fn g_spmm = nullptr;            // the entry points of the library that binding.py has loaded
 conv2d_fn g_conv2d = nullptr;
@@ -42,6 +49,13 @@ kv_read_fn g_kv_read = nullptr;
 kv_workspace_fn g_kv_workspace = nullptr;
 kv_attention_fn g_kv_attention = nullptr;
 window_attention_fn g_window_attention = nullptr;
+norm_rotate_fn g_norm_rotate = nullptr;
+shared_workspace_fn g_shared_workspace = nullptr;
+shared_attention_fn g_shared_attention = nullptr;
+pages_workspace_fn g_pages_workspace = nullptr;
+kv_extend_fn g_kv_extend = nullptr;
+kv_fork_fn g_kv_fork = nullptr;
+kv_compact_fn g_kv_compact = nullptr;
 PyObject* g_raw_stream = nullptr;    // device index -> current stream's handle
 
 struct Plan {
@@ -393,6 +407,265 @@ PyObject* window_attention(PyObject*, PyObject* const* args, Py_ssize_t n)
     });
 }
 
+// ---- what lies around a shared cache
+
+// a rows x width table of pages (rows, width < 0: any, one or more) and its leading dimension
+bool table_of(PyObject* o, int device, int64_t rows, int64_t width, const at::Tensor*& t, int64_t& ld)
+{
+    if (!plain(o, device, t) || t->scalar_type() != at::kInt || t->dim() != 2) return false;
+    const int64_t r = t->size(0), w = t->size(1);
+    if (r < 1 || w < 1 || r > INT32_MAX || w > INT32_MAX || (rows >= 0 && r != rows) || (width >= 0 && w != width)) return false;
+    if ((w > 1 && t->stride(1) != 1) || (r > 1 && t->stride(0) < w)) return false;
+    ld = r > 1 ? t->stride(0) : w;
+    return true;
+}
+at::Tensor empty_ints(int64_t n, int device)
+{
+    return at::empty({n}, at::TensorOptions().dtype(at::kInt).device(c10::Device(c10::DeviceType::CUDA, (c10::DeviceIndex)device)));
+}
+// a tuple of the tensors
+template <class... T>
+PyObject* wrapped(const T&... t)
+{
+    PyObject* items[] = {THPVariable_Wrap(t)...};
+    PyObject* all = PyTuple_New(sizeof...(T));
+    for (size_t i = 0; i < sizeof...(T); ++i) {
+        if (!items[i]) Py_CLEAR(all);
+        if (all) PyTuple_SET_ITEM(all, i, items[i]);
+        else Py_XDECREF(items[i]);
+    }
+    return all;
+}
+
+// norm_rotate(q, k, head_dim, positions, frequencies, axes, q_weight, k_weight, eps, norm, interleaved, q_out, k_out) -> (q, k), a status below zero, or None
+PyObject* norm_rotate(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (n != 13) {
+        PyErr_SetString(PyExc_TypeError, "norm_rotate(q, k, head_dim, positions, frequencies, axes, q_weight, k_weight, eps, norm, interleaved, q_out, k_out)");
+        return nullptr;
+    }
+    return guarded([&]() -> PyObject* {
+        const at::Tensor *q, *k, *p, *f, *out[2] = {nullptr, nullptr};
+        if (!THPVariable_CheckExact(args[0])) Py_RETURN_NONE;
+        const int device = THPVariable_Unpack(args[0]).device().index();
+        if (!plain(args[0], device, q) || !plain(args[1], device, k) || !plain(args[3], device, p) || !plain(args[4], device, f) || !may_allocate(device)) Py_RETURN_NONE;
+        const c10::ScalarType dt = q->scalar_type();
+        shflbw_rotation r = {};
+        if ((dt != at::kHalf && dt != at::kBFloat16) || q->dim() != 2 || k->dim() != 2 || !small_int(args[2], r.head_dim) || r.head_dim < 1) Py_RETURN_NONE;
+        const int64_t rows = q->size(0), key_rows = k->size(0), tokens = q->size(1);
+        int64_t ldq, ldk, ldqo = tokens, ldko = tokens;
+        if (rows < 1 || key_rows < 1 || rows % r.head_dim || key_rows % r.head_dim || rows / r.head_dim > INT32_MAX || key_rows / r.head_dim > INT32_MAX) Py_RETURN_NONE;
+        if (!columns(args[0], device, dt, rows, -1, q, ldq) || !columns(args[1], device, dt, key_rows, tokens, k, ldk)) Py_RETURN_NONE;
+        if (f->scalar_type() != at::kDouble || f->dim() != 1 || !f->is_contiguous() || 2 * f->size(0) > r.head_dim) Py_RETURN_NONE;
+        r.pairs = (int32_t)f->size(0);
+        if (p->scalar_type() != at::kInt || (p->dim() != 1 && p->dim() != 2) || p->size(-1) != tokens || (tokens > 1 && p->stride(-1) != 1)) Py_RETURN_NONE;
+        const int64_t position_rows = p->dim() == 2 ? p->size(0) : 1, ldp = position_rows > 1 ? p->stride(0) : tokens;
+        if (position_rows < 1 || position_rows > INT32_MAX || ldp < tokens) Py_RETURN_NONE;
+        r.position_rows = (int32_t)position_rows;
+        if (args[5] != Py_None) {
+            r.axes = indices(args[5], device, r.pairs);
+            if (!r.axes) Py_RETURN_NONE;
+        } else if (position_rows > 1) {
+            Py_RETURN_NONE;
+        }
+        if (!PyFloat_CheckExact(args[8]) || !PyBool_Check(args[9]) || !PyBool_Check(args[10])) Py_RETURN_NONE;
+        r.eps = PyFloat_AS_DOUBLE(args[8]);
+        r.norm = args[9] == Py_True;
+        r.interleaved = args[10] == Py_True;
+        for (int i = 0; i < 2; ++i) {
+            if (args[6 + i] == Py_None) continue;
+            const at::Tensor* w;
+            if (!r.norm || !plain(args[6 + i], device, w) || w->scalar_type() != dt || w->dim() != 1 || w->size(0) != r.head_dim || !w->is_contiguous()) Py_RETURN_NONE;
+            (i ? r.k_weight : r.q_weight) = w->const_data_ptr();
+        }
+        if (args[11] != Py_None && !columns(args[11], device, dt, rows, tokens, out[0], ldqo)) Py_RETURN_NONE;
+        if (args[12] != Py_None && !columns(args[12], device, dt, key_rows, tokens, out[1], ldko)) Py_RETURN_NONE;
+        r.dtype = dt == at::kBFloat16 ? SHFLBW_BF16 : SHFLBW_F16;
+        r.frequencies = static_cast<const double*>(f->const_data_ptr());
+        at::Tensor qo = out[0] ? *out[0] : empty(rows, tokens, dt, device), ko = out[1] ? *out[1] : empty(key_rows, tokens, dt, device);
+        const int32_t* pp = static_cast<const int32_t*>(p->const_data_ptr());
+        const void *qp = q->const_data_ptr(), *kp = k->const_data_ptr();
+        void *qop = qo.data_ptr(), *kop = ko.data_ptr(), *stream;
+        if (!current_stream(stream)) return nullptr;
+        const int rc = unlocked([&] {
+            return g_norm_rotate(&r, pp, ldp, qp, ldq, (int)(rows / r.head_dim), kp, ldk, (int)(key_rows / r.head_dim), qop, ldqo, kop, ldko, tokens, stream);
+        });
+        return rc < 0 ? PyLong_FromLong(rc) : wrapped(qo, ko);
+    });
+}
+
+// shared_attention(plan, q, prefix_table, prefix_lengths, table, lengths, members, starts, max_queries, max_length, max_prefix, max_sharing, out) -> out,
+// a status below zero, or None
+PyObject* shared_attention(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (n != 13) {
+        PyErr_SetString(PyExc_TypeError, "shared_attention(plan, q, prefix_table, prefix_lengths, table, lengths, members, starts, max_queries, max_length, max_prefix, "
+                                         "max_sharing, out)");
+        return nullptr;
+    }
+    const CachePlan* c = static_cast<const CachePlan*>(PyCapsule_GetPointer(args[0], CACHE_PLAN));
+    if (!c) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const at::Tensor *q, *pt, *table, *given = nullptr;
+        if (!plain(args[1], c->device, q) || q->dim() != 2 || !may_allocate(c->device)) Py_RETURN_NONE;
+        const int64_t rows = q->size(0), tokens = q->size(1), key_rows = (int64_t)c->cache.heads * c->cache.head_dim;
+        int64_t ldq, ldo = tokens;
+        if (rows < 1 || rows % key_rows || rows / c->cache.head_dim > INT32_MAX || !columns(args[1], c->device, c->dtype, rows, -1, q, ldq)) Py_RETURN_NONE;
+        shflbw_kv_prefixes p = {};
+        shflbw_kv_sequences s = {};
+        if (!table_of(args[2], c->device, -1, -1, pt, p.table_ld) || !table_of(args[4], c->device, -1, -1, table, s.table_ld)) Py_RETURN_NONE;
+        const int64_t prefixes = pt->size(0), batch = table->size(0);
+        p.prefixes = (int32_t)prefixes;
+        p.table_pages = (int32_t)pt->size(1);
+        p.lengths = indices(args[3], c->device, prefixes);
+        s.batch = (int32_t)batch;
+        s.table_pages = (int32_t)table->size(1);
+        s.lengths = indices(args[5], c->device, batch);
+        if (!p.lengths || !s.lengths) Py_RETURN_NONE;
+        if (args[6] != Py_None) {
+            p.members = indices(args[6], c->device, prefixes + 1);
+            if (!p.members) Py_RETURN_NONE;
+        } else if (prefixes != 1) {
+            Py_RETURN_NONE;
+        }
+        int most[3] = {0, 0, 0};                           // max_length, max_prefix, max_sharing
+        if (!small_int(args[8], s.max_queries) || s.max_queries < 0) Py_RETURN_NONE;
+        for (int i = 0; i < 3; ++i)
+            if (args[9 + i] != Py_None && (!small_int(args[9 + i], most[i]) || most[i] < 0)) Py_RETURN_NONE;
+        if (args[7] != Py_None) {
+            s.starts = indices(args[7], c->device, batch + 1);
+            if (!s.starts) Py_RETURN_NONE;
+        } else if (tokens != batch || s.max_queries != 1) {
+            Py_RETURN_NONE;
+        }
+        if (args[12] != Py_None && !columns(args[12], c->device, c->dtype, rows, tokens, given, ldo)) Py_RETURN_NONE;
+        s.q_heads = (int32_t)(rows / c->cache.head_dim);
+        s.tokens = tokens;
+        s.max_length = args[9] == Py_None ? (int64_t)s.table_pages * c->cache.page_tokens : most[0];
+        p.max_length = args[10] == Py_None ? (int64_t)p.table_pages * c->cache.page_tokens : most[1];
+        p.max_tokens = args[11] == Py_None ? tokens : most[2];
+        s.table = static_cast<const int32_t*>(table->const_data_ptr());
+        p.table = static_cast<const int32_t*>(pt->const_data_ptr());
+        const int64_t bytes = g_shared_workspace(&c->cache, &p, &s);
+        if (bytes < 0) return PyLong_FromLong((long)bytes);
+        at::Tensor out = given ? *given : empty(rows, tokens, c->dtype, c->device), work;
+        if (bytes) work = empty(1, bytes, at::kByte, c->device);
+        const void* qp = q->const_data_ptr();
+        void *op = out.data_ptr(), *wp = bytes ? work.data_ptr() : nullptr, *stream;
+        if (!current_stream(stream)) return nullptr;
+        const int rc = unlocked([&] { return g_shared_attention(&c->cache, &p, &s, qp, ldq, op, ldo, wp, bytes, stream); });
+        return rc < 0 ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
+    });
+}
+
+// What the three calls on pages have in common: the tables, lengths (rows of `in`; none where lengths is nullptr) and uses of both sides.  out: None, or a
+// tuple of the results' tensors.
+struct PageSides {
+    shflbw_kv_pages in = {}, out = {};
+    at::Tensor table, lengths, uses, work;
+    int64_t bytes = 0;
+};
+bool page_sides(const CachePlan* c, PyObject* table, PyObject* lengths, PyObject* uses, PyObject* out, int64_t rows, PageSides& s)
+{
+    const at::Tensor *t, *given = nullptr;
+    if (!may_allocate(c->device) || !table_of(table, c->device, -1, -1, t, s.in.table_ld)) return false;
+    const int64_t pages = c->cache.pages, width = t->size(1);
+    s.in.sequences = (int32_t)t->size(0);
+    if (rows < 0) rows = s.in.sequences;
+    if (rows < 1 || rows > INT32_MAX) return false;
+    s.out.sequences = (int32_t)rows;
+    s.in.table_pages = s.out.table_pages = (int32_t)width;
+    s.in.table = const_cast<int32_t*>(static_cast<const int32_t*>(t->const_data_ptr()));
+    s.in.uses = const_cast<int32_t*>(indices(uses, c->device, pages));
+    if (!s.in.uses) return false;
+    if (lengths) {
+        s.in.lengths = const_cast<int32_t*>(indices(lengths, c->device, s.in.sequences));
+        if (!s.in.lengths) return false;
+    }
+    s.out.table_ld = width;
+    if (out == Py_None) {
+        s.table = empty(rows, width, at::kInt, c->device);
+        s.uses = empty_ints(pages, c->device);
+        if (lengths) s.lengths = empty_ints(rows, c->device);
+    } else {
+        const Py_ssize_t last = lengths ? 2 : 1;
+        if (!PyTuple_CheckExact(out) || PyTuple_GET_SIZE(out) != last + 1) return false;
+        if (!table_of(PyTuple_GET_ITEM(out, 0), c->device, rows, width, given, s.out.table_ld)) return false;
+        s.table = *given;
+        if (!indices(PyTuple_GET_ITEM(out, last), c->device, pages)) return false;
+        s.uses = THPVariable_Unpack(PyTuple_GET_ITEM(out, last));
+        if (lengths) {
+            if (!indices(PyTuple_GET_ITEM(out, 1), c->device, rows)) return false;
+            s.lengths = THPVariable_Unpack(PyTuple_GET_ITEM(out, 1));
+        }
+    }
+    s.out.table = static_cast<int32_t*>(s.table.data_ptr());
+    s.out.uses = static_cast<int32_t*>(s.uses.data_ptr());
+    if (lengths) s.out.lengths = static_cast<int32_t*>(s.lengths.data_ptr());
+    s.bytes = g_pages_workspace(&c->cache, (int)(rows > s.in.sequences ? rows : s.in.sequences));
+    if (s.bytes < 0) return false;
+    s.work = empty(1, s.bytes, at::kByte, c->device);
+    return true;
+}
+
+// kv_extend(plan, table, lengths, uses, counts, tokens, out, slots, starts) -> (table, lengths, uses, slots, starts), a status below zero, or None
+PyObject* kv_extend(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (n != 9) { PyErr_SetString(PyExc_TypeError, "kv_extend(plan, table, lengths, uses, counts, tokens, out, slots, starts)"); return nullptr; }
+    const CachePlan* c = static_cast<const CachePlan*>(PyCapsule_GetPointer(args[0], CACHE_PLAN));
+    if (!c) return nullptr;
+    return guarded([&]() -> PyObject* {
+        PageSides s;
+        int tokens;
+        if (!small_int(args[5], tokens) || tokens < 0 || !page_sides(c, args[1], args[2], args[3], args[6], -1, s)) Py_RETURN_NONE;
+        const int32_t* counts = indices(args[4], c->device, s.in.sequences);
+        if (!counts || (args[7] != Py_None && !indices(args[7], c->device, tokens)) || (args[8] != Py_None && !indices(args[8], c->device, s.in.sequences + 1LL)))
+            Py_RETURN_NONE;
+        at::Tensor slots = args[7] != Py_None ? THPVariable_Unpack(args[7]) : empty_ints(tokens, c->device);
+        at::Tensor starts = args[8] != Py_None ? THPVariable_Unpack(args[8]) : empty_ints(s.in.sequences + 1LL, c->device);
+        int32_t *sp = static_cast<int32_t*>(slots.data_ptr()), *tp = static_cast<int32_t*>(starts.data_ptr());
+        void *wp = s.work.data_ptr(), *stream;
+        if (!current_stream(stream)) return nullptr;
+        const int rc = unlocked([&] { return g_kv_extend(&c->cache, &s.in, &s.out, counts, sp, tp, tokens, wp, s.bytes, stream); });
+        return rc < 0 ? PyLong_FromLong(rc) : wrapped(s.table, s.lengths, s.uses, slots, starts);
+    });
+}
+
+// kv_fork(plan, table, lengths, uses, parents, out) -> (table, lengths, uses), a status below zero, or None
+PyObject* kv_fork(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (n != 6) { PyErr_SetString(PyExc_TypeError, "kv_fork(plan, table, lengths, uses, parents, out)"); return nullptr; }
+    const CachePlan* c = static_cast<const CachePlan*>(PyCapsule_GetPointer(args[0], CACHE_PLAN));
+    if (!c) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const at::Tensor* who;
+        if (!plain(args[4], c->device, who) || who->dim() != 1 || who->size(0) < 1) Py_RETURN_NONE;
+        const int32_t* parents = indices(args[4], c->device, who->size(0));
+        PageSides s;
+        if (!parents || !page_sides(c, args[1], args[2], args[3], args[5], who->size(0), s)) Py_RETURN_NONE;
+        void *wp = s.work.data_ptr(), *stream;
+        if (!current_stream(stream)) return nullptr;
+        const int rc = unlocked([&] { return g_kv_fork(&c->cache, &s.in, &s.out, parents, wp, s.bytes, stream); });
+        return rc < 0 ? PyLong_FromLong(rc) : wrapped(s.table, s.lengths, s.uses);
+    });
+}
+
+// kv_compact(plan, table, uses, out) -> (table, uses), a status below zero, or None
+PyObject* kv_compact(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (n != 4) { PyErr_SetString(PyExc_TypeError, "kv_compact(plan, table, uses, out)"); return nullptr; }
+    const CachePlan* c = static_cast<const CachePlan*>(PyCapsule_GetPointer(args[0], CACHE_PLAN));
+    if (!c) return nullptr;
+    return guarded([&]() -> PyObject* {
+        PageSides s;
+        if (!page_sides(c, args[1], nullptr, args[2], args[3], -1, s)) Py_RETURN_NONE;
+        void *wp = s.work.data_ptr(), *stream;
+        if (!current_stream(stream)) return nullptr;
+        const int rc = unlocked([&] { return g_kv_compact(&c->cache, &s.in, &s.out, wp, s.bytes, stream); });
+        return rc < 0 ? PyLong_FromLong(rc) : wrapped(s.table, s.uses);
+    });
+}
+
 // cache_plan(data, pages, page_tokens, heads, head_dim, bf16, device index) -> capsule
 PyObject* cache_plan(PyObject*, PyObject* args)
 {
@@ -417,6 +690,21 @@ PyObject* connect_attention(PyObject*, PyObject* args)
     g_kv_workspace = reinterpret_cast<kv_workspace_fn>((uintptr_t)s);
     g_kv_attention = reinterpret_cast<kv_attention_fn>((uintptr_t)a);
     g_window_attention = reinterpret_cast<window_attention_fn>((uintptr_t)p);
+    Py_RETURN_NONE;
+}
+
+// connect_serving(addresses of shflbw_norm_rotate, _kv_shared_attention_workspace, _kv_shared_attention, _kv_pages_workspace, _kv_extend, _kv_fork, _kv_compact), after connect
+PyObject* connect_serving(PyObject*, PyObject* args)
+{
+    unsigned long long r, w, a, p, e, f, c;
+    if (!PyArg_ParseTuple(args, "KKKKKKK", &r, &w, &a, &p, &e, &f, &c)) return nullptr;
+    g_norm_rotate = reinterpret_cast<norm_rotate_fn>((uintptr_t)r);
+    g_shared_workspace = reinterpret_cast<shared_workspace_fn>((uintptr_t)w);
+    g_shared_attention = reinterpret_cast<shared_attention_fn>((uintptr_t)a);
+    g_pages_workspace = reinterpret_cast<pages_workspace_fn>((uintptr_t)p);
+    g_kv_extend = reinterpret_cast<kv_extend_fn>((uintptr_t)e);
+    g_kv_fork = reinterpret_cast<kv_fork_fn>((uintptr_t)f);
+    g_kv_compact = reinterpret_cast<kv_compact_fn>((uintptr_t)c);
     Py_RETURN_NONE;
 }
 
@@ -463,6 +751,12 @@ PyMethodDef methods[] = {
     {"kv_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&kv_read)), METH_FASTCALL, "shflbw_kv_read on plain tensors."},
     {"kv_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&kv_attention)), METH_FASTCALL, "shflbw_kv_attention on plain tensors."},
     {"window_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&window_attention)), METH_FASTCALL, "shflbw_window_attention on plain tensors."},
+    {"connect_serving", connect_serving, METH_VARARGS, "The entry points around a shared cache of the loaded library."},
+    {"norm_rotate", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&norm_rotate)), METH_FASTCALL, "shflbw_norm_rotate on plain tensors."},
+    {"shared_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&shared_attention)), METH_FASTCALL, "shflbw_kv_shared_attention on plain tensors."},
+    {"kv_extend", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&kv_extend)), METH_FASTCALL, "shflbw_kv_extend on plain tensors."},
+    {"kv_fork", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&kv_fork)), METH_FASTCALL, "shflbw_kv_fork on plain tensors."},
+    {"kv_compact", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&kv_compact)), METH_FASTCALL, "shflbw_kv_compact on plain tensors."},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -140,7 +140,8 @@ def book_of(rng, pages, page, width, rows, fill=0.5, shared=True):
     return Book(pages, page, width, out)
 
 
-@pytest.mark.parametrize("pages,page,width,rows", [(1, 32, 1, 1), (40, 32, 5, 9), (300, 64, 7, 33), (4097, 32, 40, 130), (9000, 128, 3, 1500)])
+@pytest.mark.parametrize("pages,page,width,rows", [(1, 32, 1, 1), (40, 32, 5, 9), (300, 64, 7, 33), (4097, 32, 40, 130), (9000, 128, 3, 1500),
+                                                   (16385, 32, 4, 60), (16384, 32, 30, 1100), (20000, 64, 2, 2500)])
 @pytest.mark.parametrize("seed", [0, 1])
 def test_extend(pages, page, width, rows, seed):
     announce("extend", pages, page, width, rows, seed)
@@ -185,7 +186,8 @@ def test_extend_at_the_end_of_things():
 
 
 @pytest.mark.parametrize("pages,page,width,rows,children,heads,D", [(1, 32, 1, 1, 1, 1, 64), (40, 32, 5, 9, 12, 3, 96), (300, 64, 7, 33, 20, 5, 128),
-                                                                    (4097, 32, 40, 130, 257, 1, 64), (9000, 32, 3, 1500, 1400, 1, 64)])
+                                                                    (4097, 32, 40, 130, 257, 1, 64), (9000, 32, 3, 1500, 1400, 1, 64),
+                                                                    (16385, 32, 4, 60, 70, 1, 64), (16384, 32, 30, 700, 800, 1, 64), (9000, 32, 2, 2500, 2049, 1, 64)])
 @pytest.mark.parametrize("seed", [0, 1])
 def test_fork(pages, page, width, rows, children, heads, D, seed):
     announce("fork", pages, page, width, rows, children, seed)
@@ -234,7 +236,7 @@ def test_fork_at_the_end_of_things():
     assert got[0].tolist() == book.table() == [[0], [1]] and got[2].tolist() == [1, 1] and torch.equal(c2.data[1], before[0])
 
 
-@pytest.mark.parametrize("pages,page,width,rows,heads,D", [(1, 32, 1, 1, 1, 64), (40, 32, 5, 9, 3, 96), (300, 64, 7, 33, 5, 128), (4096, 32, 40, 130, 1, 64),
+@pytest.mark.parametrize("pages,page,width,rows,heads,D", [(1, 32, 1, 1, 1, 64), (40, 32, 5, 9, 3, 96), (300, 64, 7, 33, 5, 128), (4096, 32, 40, 130, 1, 64), (16384, 32, 3, 5, 1, 64), (20481, 32, 40, 900, 1, 64),
                                                            (9001, 32, 6, 1500, 2, 64)])
 @pytest.mark.parametrize("share", [0.0, 0.1, 0.6, 1.0])
 def test_compact(pages, page, width, rows, heads, D, share):
