@@ -403,7 +403,7 @@ typedef struct {
     const int32_t *table, *lengths, *members;
 } shflbw_kv_prefixes;
 
-/* Bytes of device workspace that shflbw_kv_shared_attention needs (the pointers of the structs are not followed), or a negative status. */
+/* Bytes of device workspace that shflbw_kv_shared_attention needs (may be 0; the pointers of the structs are not followed), or a negative status. */
 int64_t shflbw_kv_shared_attention_workspace(const shflbw_kv_cache* cache, const shflbw_kv_prefixes* prefixes, const shflbw_kv_sequences* sequences);
 
 /*
@@ -412,7 +412,7 @@ int64_t shflbw_kv_shared_attention_workspace(const shflbw_kv_cache* cache, const
  * positions are the own tokens' alone (a length of 0, or below the queries, leaves queries with the prefix).  A prefix is read once for
  * all queries of all its sequences.  window must be 0 (under a window a far prefix is not seen: shflbw_kv_attention takes its pages
  * in the sequence's table).  Columns of q before the first sequence's and behind the last one's are left as they were.
- * A workspace is always needed; everything else, accuracy included, is as in shflbw_kv_attention.
+ * Everything else, the workspace and accuracy included, is as in shflbw_kv_attention.
  */
 int shflbw_kv_shared_attention(const shflbw_kv_cache* cache, const shflbw_kv_prefixes* prefixes, const shflbw_kv_sequences* sequences,
                                const void* q, int64_t ldq, void* out, int64_t ldo, void* workspace, int64_t workspace_bytes, void* stream);

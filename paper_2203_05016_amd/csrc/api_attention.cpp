@@ -62,8 +62,9 @@ int check_prefixes(const shflbw_kv_cache* c, const shflbw_kv_prefixes* p, const 
 
 SharedPlan plan_of(const shflbw_kv_cache* c, const shflbw_kv_prefixes* p, const shflbw_kv_sequences* s)
 {
+    const bool keys_fit = ((int64_t)p->table_pages + s->table_pages) * c->page_tokens <= INT_MAX - 1024;
     return plan_shared_attention(p->prefixes, p->max_tokens, p->max_length, s->batch, c->heads, s->q_heads / c->heads, c->head_dim, s->tokens, s->max_queries,
-                                 s->max_length);
+                                 s->max_length, keys_fit);
 }
 
 // What a call over the cache gives the kernels, but for where results go
@@ -167,10 +168,29 @@ int shflbw_kv_shared_attention(const shflbw_kv_cache* cache, const shflbw_kv_pre
         return fail(SHFLBW_ERR_NULL_ARG, "q, out, tables and lengths must not be NULL");
     if (ldq < s->tokens || ldo < s->tokens) return fail(SHFLBW_ERR_BAD_SHAPE, "leading dimension too small");
     const SharedPlan plan = plan_of(cache, prefixes, s);
-    if (plan.workspace > workspace_bytes || !workspace) return fail(SHFLBW_ERR_NULL_ARG, "the call needs a workspace of %lld bytes", (long long)plan.workspace);
-    if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(SHFLBW_ERR_BAD_SHAPE, "the workspace must be 16-byte aligned");
-    const int64_t rows = (int64_t)s->q_heads * s->tokens, parts = plan.prefix.splits + plan.own.splits;
-    AttnArgs own = cache_args(cache, s, plan.own, q, ldq), prefix = cache_args(cache, s, plan.prefix, q, ldq);
+    if (plan.workspace > workspace_bytes || (plan.workspace && !workspace)) return fail(SHFLBW_ERR_NULL_ARG, "the call needs a workspace of %lld bytes", (long long)plan.workspace);
+    if (plan.workspace && reinterpret_cast<uintptr_t>(workspace) % 16) return fail(SHFLBW_ERR_BAD_SHAPE, "the workspace must be 16-byte aligned");
+    const int64_t rows = (int64_t)s->q_heads * s->tokens, parts = plan.prefix.splits + (plan.joins ? 0 : plan.own.splits);
+    AttnArgs own = cache_args(cache, s, plan.own, q, ldq);
+    own.out = static_cast<uint16_t*>(out);
+    own.ldo = ldo;
+    if (plan.behind) {
+        own.behind = true;
+        own.members = prefixes->members;
+        own.prefix_table = prefixes->table;
+        own.prefix_lengths = prefixes->lengths;
+        own.prefix_ld = prefixes->table_ld;
+        own.prefix_width = prefixes->table_pages;
+        own.prefixes = prefixes->prefixes;
+        own.sequences = s->batch;
+        if (plan.own.splits > 1) {
+            own.part_o = static_cast<float*>(workspace);
+            own.part_ml = own.part_o + parts * rows * cache->head_dim;
+        }
+        return cache->dtype == SHFLBW_BF16 ? run_attention_bf16(own, plan.own, cache->head_dim, false, stream)
+                                           : run_attention_f16(own, plan.own, cache->head_dim, false, stream);
+    }
+    AttnArgs prefix = cache_args(cache, s, plan.prefix, q, ldq);
     prefix.table = prefixes->table;
     prefix.lengths = prefixes->lengths;
     prefix.table_ld = prefixes->table_ld;
@@ -179,12 +199,18 @@ int shflbw_kv_shared_attention(const shflbw_kv_cache* cache, const shflbw_kv_pre
     prefix.shared = true;
     prefix.members = prefixes->members;
     prefix.sequences = s->batch;
-    prefix.out = own.out = static_cast<uint16_t*>(out);
-    prefix.ldo = own.ldo = ldo;
+    prefix.out = own.out;
+    prefix.ldo = ldo;
     prefix.part_o = static_cast<float*>(workspace);
     prefix.part_ml = prefix.part_o + parts * rows * cache->head_dim;
-    own.part_o = prefix.part_o + plan.prefix.splits * rows * cache->head_dim;
-    own.part_ml = prefix.part_ml + 2 * plan.prefix.splits * rows;
+    if (plan.joins) {
+        own.joined_o = prefix.part_o;
+        own.joined_ml = prefix.part_ml;
+        own.joined = plan.prefix.splits;
+    } else {
+        own.part_o = prefix.part_o + plan.prefix.splits * rows * cache->head_dim;
+        own.part_ml = prefix.part_ml + 2 * plan.prefix.splits * rows;
+    }
     return cache->dtype == SHFLBW_BF16 ? run_shared_attention_bf16(prefix, own, plan, cache->head_dim, stream)
                                        : run_shared_attention_f16(prefix, own, plan, cache->head_dim, stream);
 }

@@ -64,7 +64,16 @@ struct AttnArgs {
     bool shared;
     const int32_t* members;
     int sequences;            // of `starts`
+    // Sequences behind prefixes (the tile kernel): their keys are the prefix's, from 0 on, and their own, from the next multiple of a tile on
+    bool behind;
+    const int32_t *prefix_table, *prefix_lengths;
+    int64_t prefix_ld;
+    int prefix_width, prefixes;
+    // Parts of other keys (prefixes') to be joined with what the decoding kernel finds: `joined` of them, up to ATTN_JOINED, as part_o and part_ml
+    const float *joined_o, *joined_ml;
+    int joined;
 };
+constexpr int ATTN_JOINED = 32;
 
 // Wavefronts per SIMD of the decoding kernel that the plan counts on.  Its registers allow no more, but for heads of 64 with 32 and 48
 // columns, which compile to 119 and 155: 4 and 3 would fit.
@@ -117,13 +126,16 @@ constexpr bool tile_kernel_exists(int D, bool cache, int waves, bool tiny)
     return tiny ? !cache && waves == 4 : waves == 4 || (waves == 8 && (cache || D > 64));
 }
 
-// Attention over shared prefixes: the prefixes' part, the sequences' own part, and the workspace of all parts
+// Attention over shared prefixes: the prefixes' part and the sequences' own part; or (behind) both at once, as `own`.  workspace: of all parts
 struct SharedPlan {
     AttnPlan prefix, own;
+    bool behind;
+    bool joins;               // the own part's kernel joins the prefixes' parts
     int64_t workspace;
 };
+// keys_fit: a sequence's keys behind its prefix's are counted in 32 bits
 SharedPlan plan_shared_attention(int prefixes, int64_t max_sharing, int64_t max_prefix, int batch, int heads, int group, int D, int64_t tokens, int max_queries,
-                                 int64_t max_length);
+                                 int64_t max_length, bool keys_fit);
 
 // SHFLBW_OK, or why the cache cannot be used (host checks of its fields)
 int check_cache(const shflbw_kv_cache* cache);

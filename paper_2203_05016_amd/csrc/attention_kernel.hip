@@ -115,6 +115,9 @@ __device__ __forceinline__ uint2 attn_transposed(attn_lds p)
 typedef const __attribute__((address_space(4))) int32_t* attn_table;
 __device__ __forceinline__ attn_table attn_scalar(const int32_t* p) { return (attn_table)(uintptr_t)p; }
 
+// The row among parts' of a column whose head is in the upper and whose token in the lower 32 bits
+__device__ __forceinline__ int64_t attn_row(const AttnArgs& a, int64_t where) { return (where >> 32) * a.tokens + (where & 0xffffffffLL); }
+
 // One sequence of a call
 struct AttnSeq {
     int64_t t0;    // its first column of q
@@ -153,6 +156,20 @@ __device__ __forceinline__ AttnSeq attn_sequence(const AttnArgs& a, int b)
         s.len = s.nq;
     }
     return s;
+}
+
+// The prefix that sequence b stands behind: its row, or -1
+__device__ __forceinline__ int attn_prefix_of(const AttnArgs& a, int b)
+{
+    if (!a.members) return 0;
+    const attn_table members = attn_scalar(a.members);
+    int low = 0, high = a.prefixes;                        // members[low] <= b < members[high], where there is such a row
+    while (high - low > 1) {
+        const int mid = low + (high - low) / 2;
+        if (members[mid] <= b) low = mid;
+        else high = mid;
+    }
+    return members[low] <= b && b < members[low + 1] ? low : -1;
 }
 
 // The tiles of keys (shifted by `shift`: tile t holds keys tile * t - shift and up) that queries at positions first..last need: those of
@@ -218,6 +235,11 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
     __shared__ __attribute__((aligned(16))) char smem[BYTES];
     __shared__ float stat[W][C][2];
     __shared__ int64_t where[C];
+    // Of 16 columns: what is joined with their sums is weighted by (own: 16 x 2 maxima and sums, behind them)
+    constexpr int J_AT = (O_BYTES + 15) / 16 * 16, J_BYTES = (16 * (ATTN_JOINED + 1) + 32) * 4;
+    static_assert(J_AT + J_BYTES <= BYTES, "the weights of joined parts lie behind the sums");
+    float* weight = reinterpret_cast<float*>(smem + J_AT);
+    float* own = weight + 16 * (ATTN_JOINED + 1);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int quarter = lane >> 4, r = lane & 15;
@@ -307,7 +329,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
 #pragma unroll
             for (int k = 0; k < D / (W * FS); ++k) *reinterpret_cast<uint16_t*>(smem + c * QP + (f0 + k * W * FS) * 2) = real ? x[k] : 0;
         // where a column's results go: head and token
-        if (wave == 0 && n < C) where[c] = !a.part_o ? (int64_t)(h * a.group + g) * D * a.ldo + seq.t0 + i
+        if (wave == 0 && n < C) where[c] = a.joined ? (int64_t)(h * a.group + g) << 32 | (seq.t0 + i) : !a.part_o ? (int64_t)(h * a.group + g) * D * a.ldo + seq.t0 + i
                                                          : ((int64_t)split * a.heads * a.group + h * a.group + g) * a.tokens + seq.t0 + i;
         __syncthreads();
 #pragma unroll
@@ -465,7 +487,12 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
         for (int i = 0; i < W; ++i) total += stat[i][col][1] * attn_exp2(stat[i][col][0] - top);
         if (seq.bad) total = __builtin_nanf("");
         float f = attn_exp2(m[n] - top);
-        if (!a.part_o) f = p[n] < 0 ? 0 : f / total;
+        if (a.joined) {
+            if (wave == 0 && quarter == 0) {
+                own[2 * r] = p[n] < 0 ? -INFINITY : top;
+                own[2 * r + 1] = total;
+            }
+        } else if (!a.part_o) f = p[n] < 0 ? 0 : f / total;
         else if (seq.bad) f = total;
         if (a.part_o && wave == 0 && quarter == 0 && col < cols) {
             const int64_t row = where[col];
@@ -475,6 +502,28 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
 #pragma unroll
         for (int t = 0; t < DT; ++t) *reinterpret_cast<float4v*>(sums + (wave * 16 + r) * OP + 16 * t + 4 * quarter) = o[n][t] * f;
         __syncthreads();
+        if (a.joined) {
+            // 32 lanes to a column, one to a part
+            for (int c = threadIdx.x >> 5; c < 16 && 16 * n + c < cols; c += 2 * W) {
+                const int part = threadIdx.x & 31;
+                const int64_t row = attn_row(a, where[16 * n + c]) + (int64_t)part * a.heads * a.group * a.tokens;
+                const bool has = part < a.joined;
+                const float m_part = has ? a.joined_ml[2 * row] : -INFINITY, l_part = has ? a.joined_ml[2 * row + 1] : 0;
+                float most = m_part;
+#pragma unroll
+                for (int by = 1; by < 32; by *= 2) most = fmaxf(most, __shfl_xor(most, by));
+                most = fmaxf(most, own[2 * c]);
+                const bool none = most == -INFINITY;           // nothing is seen
+                const float w_part = none ? 0 : attn_exp2(m_part - most), w_own = none ? 0 : attn_exp2(own[2 * c] - most);
+                float sum = l_part * w_part;
+#pragma unroll
+                for (int by = 1; by < 32; by *= 2) sum += __shfl_xor(sum, by);
+                sum += own[2 * c + 1] * w_own;
+                if (has) weight[c * (ATTN_JOINED + 1) + part] = none ? 0 : w_part / sum;
+                if (part == 0) weight[c * (ATTN_JOINED + 1) + ATTN_JOINED] = none ? 0 : w_own / sum;
+            }
+            __syncthreads();
+        }
 #pragma unroll
         for (int k = 0; k < 16 * D / (64 * W); ++k) {
             const int e = threadIdx.x + k * 64 * W, c = e / D, d = e % D, at = 16 * n + c;
@@ -482,7 +531,16 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
             float x = 0;
 #pragma unroll
             for (int i = 0; i < W; ++i) x += sums[(i * 16 + c) * OP + d];
-            if (!a.part_o) a.out[where[at] + d * a.ldo] = attn_narrow<BF>(x);
+            if (a.joined) {
+                const float* w = weight + c * (ATTN_JOINED + 1);
+                const float* from = a.joined_o + attn_row(a, where[at]) * D + d;
+                const int64_t step = (int64_t)a.heads * a.group * a.tokens * D;
+                x *= w[ATTN_JOINED];
+#pragma unroll 8
+                for (int i = 0; i < a.joined; ++i, from += step) x += *from * w[i];
+            }
+            if (a.joined) a.out[((where[at] >> 32) * D + d) * a.ldo + (where[at] & 0xffffffffLL)] = attn_narrow<BF>(x);
+            else if (!a.part_o) a.out[where[at] + d * a.ldo] = attn_narrow<BF>(x);
             else a.part_o[where[at] * D + d] = x;
         }
         __syncthreads();
@@ -614,32 +672,65 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
     const int blk = a.col_blocks - 1 - inner / a.splits, split = inner % a.splits;
     const int b = pair / a.heads, h = pair % a.heads;
 
-    const AttnSeq seq = attn_sequence<CACHE>(a, b);
-    const int blocks = (seq.nq + ATTN_TILE_QUERIES - 1) / ATTN_TILE_QUERIES;
-    const int64_t items = (int64_t)blocks * a.group, item0 = (int64_t)blk * W;
+    AttnSeq seq = attn_sequence<CACHE>(a, b);
+    // A prefix's queries are taken as they come, 32 columns of all of the group's heads at a time: all see the same keys
+    const bool flat = CACHE && a.shared;
+    const int64_t columns = (int64_t)seq.nq * a.group;
+    const int64_t items = flat ? (columns + ATTN_TILE_QUERIES - 1) / ATTN_TILE_QUERIES : (int64_t)((seq.nq + ATTN_TILE_QUERIES - 1) / ATTN_TILE_QUERIES) * a.group;
+    const int64_t item0 = (int64_t)blk * W;
     if (item0 >= items) return;
     const int64_t item_last = items < item0 + W ? items - 1 : item0 + W - 1;
     const int shift = CACHE ? 0 : (int)(seq.t0 & 7);       // tiles of a prompt begin at multiples of 8 columns
-    const int p0 = seq.len - seq.nq;
-    const auto position = [&](int64_t query) { return CACHE && a.shared ? seq.len - 1 : p0 + (int)(query < seq.nq ? query : seq.nq - 1); };
+    // Behind a prefix the own keys begin at `lift`, and the first `sinks` keys, the prefix's, are seen by all
+    int lift = 0, sinks = a.sinks;
+    attn_table prefix_table = nullptr;
+    if (CACHE && a.behind) {
+        const int g = attn_prefix_of(a, b), most = a.prefix_width << a.page_shift;
+        const int length = g < 0 ? 0 : attn_scalar(a.prefix_lengths)[g];
+        seq.bad |= length > most;
+        sinks = length > most ? most : length < 0 ? 0 : length;
+        lift = (sinks + ATTN_TILE_KEYS - 1) / ATTN_TILE_KEYS * ATTN_TILE_KEYS;
+        prefix_table = attn_scalar(a.prefix_table + (g < 0 ? 0 : g) * a.prefix_ld);
+    }
+    const int p0 = lift + seq.len - seq.nq;
+    const auto position = [&](int64_t query) {
+        if (flat) return seq.len - 1;
+        const int at = p0 + (int)(query < seq.nq ? query : seq.nq - 1);
+        return CACHE && at < lift ? lift - 1 : at;         // (before all own keys: the prefix alone, or nothing)
+    };
+    const auto window_start = [&](int p) { return CACHE && a.behind ? lift : attn_window_start(p, a.window); };
     const int wg_first = position(item0 / a.group * ATTN_TILE_QUERIES);
     const int wg_last = position(item_last / a.group * ATTN_TILE_QUERIES + ATTN_TILE_QUERIES - 1);
-    const AttnTiles tiles = attn_tiles(wg_first, wg_last, a.window, a.sinks, shift, ATTN_TILE_KEYS);
+    const AttnTiles tiles = attn_tiles(wg_first, wg_last, a.window, CACHE && a.behind ? 0 : sinks, shift, ATTN_TILE_KEYS);
     const int v_begin = split * (a.splits > 1 ? a.split_tiles : 0);
     const int v_end = split + 1 == a.splits || tiles.count - v_begin < a.split_tiles ? tiles.count : v_begin + a.split_tiles;   // (as in the other kernel)
 
     // the wavefront's item; one that is not there repeats the last one, needs no keys, and its result is dropped
     const bool works = item0 + wave <= item_last;
     const int64_t item = works ? item0 + wave : item_last;
-    const int head = h * a.group + (int)(item % a.group), q0 = (int)(item / a.group) * ATTN_TILE_QUERIES, query = q0 + c;
-    const int p = position(query), lo = attn_window_start(p, a.window);
+    const int q0 = (int)(item / a.group) * ATTN_TILE_QUERIES;
+    struct Column {
+        int head, query;
+        bool real;
+    };
+    // (worked out where it is needed, twice)
+    const auto column = [&]() __attribute__((always_inline)) {
+        if (!flat) return Column{h * a.group + (int)(item % a.group), q0 + c, q0 + c < seq.nq};
+        // the item's first column, and from there in 32 bits
+        const int64_t col0 = item * ATTN_TILE_QUERIES;
+        const int in = col0 + c < columns ? c : (int)(columns - 1 - col0);
+        const unsigned from = (unsigned)(col0 % seq.nq) + in;
+        return Column{h * a.group + (int)(col0 / seq.nq) + (int)(from / (unsigned)seq.nq), (int)(from % (unsigned)seq.nq), col0 + c < columns};
+    };
+    const int p = position(q0 + c), lo = window_start(p);
     const int first = works ? position(q0) : INT32_MAX, last = works ? position(q0 + ATTN_TILE_QUERIES - 1) : -1;
-    const int window_first = attn_window_start(first, a.window), window_last = attn_window_start(last, a.window);
+    const int window_first = window_start(first), window_last = window_start(last);
 
     // queries: lane c has column c; features 16 s + 8 half and up
     uint4v q[S];
     {
-        const uint16_t* src = a.q + ((int64_t)head * D + 8 * half) * a.ldq + seq.t0 + (query < seq.nq ? query : seq.nq - 1);
+        const Column own = column();
+        const uint16_t* src = a.q + ((int64_t)own.head * D + 8 * half) * a.ldq + seq.t0 + (own.query < seq.nq ? own.query : seq.nq - 1);
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
@@ -651,13 +742,13 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
     const int key_sinks = -shift, key_window = (tiles.window - tiles.sinks) * ATTN_TILE_KEYS - shift;
     const auto first_key = [&](int v) __attribute__((always_inline)) { return v * ATTN_TILE_KEYS + (v < tiles.sinks ? key_sinks : key_window); };
     // whether not all of the workgroup's queries see all 64 keys from j on
-    const int wg_window = attn_window_start(wg_last, a.window);
+    const int wg_window = window_start(wg_last);
     const auto partial = [&](int j) __attribute__((always_inline)) {
-        return j < 0 || j + ATTN_TILE_KEYS - 1 > wg_first || (j < wg_window && j + ATTN_TILE_KEYS - 1 >= a.sinks);
+        return j < 0 || j + ATTN_TILE_KEYS - 1 > wg_first || (j < wg_window && j + ATTN_TILE_KEYS - 1 >= sinks);
     };
     // of 32 keys from j on: whether any of the wavefront's queries sees any, or not all see all
-    const auto is_needed = [&](int j) __attribute__((always_inline)) { return j <= last && j + 31 >= 0 && (j + 31 >= window_first || j < a.sinks); };
-    const auto is_masked = [&](int j) __attribute__((always_inline)) { return j < 0 || j + 31 > first || (j < window_last && j + 31 >= a.sinks); };
+    const auto is_needed = [&](int j) __attribute__((always_inline)) { return j <= last && j + 31 >= 0 && (j + 31 >= window_first || j < sinks); };
+    const auto is_masked = [&](int j) __attribute__((always_inline)) { return j < 0 || j + 31 > first || (j < window_last && j + 31 >= sinks); };
 
     // ---- staging: memory -> registers -> LDS, a part at a time, to be spread among the products
     const int page = 1 << a.page_shift;
@@ -690,11 +781,14 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
             lds_off[n] = (kind ? Stage::K_BYTES : 0) + f * 128 + ((member & 7) ^ attn_unit(f)) * 16;
         }
     }
+    // a tile's keys are all the prefix's or all the sequence's own; keys past the last page are hidden
+    const auto page_of = [&](int j) __attribute__((always_inline)) {
+        const bool own = j >= lift;
+        const int idx = (own ? j - lift : j) >> a.page_shift, width = own ? a.table_width : a.prefix_width;
+        return (own ? table : prefix_table)[idx < width ? idx : width - 1];
+    };
     const auto find_page = [&](int j) __attribute__((always_inline)) {
-        if constexpr (CACHE) {
-            const int idx = (j + brings * 16) >> a.page_shift;
-            page_id = table[idx < a.table_width ? idx : a.table_width - 1];   // (keys past the last page are hidden)
-        }
+        if constexpr (CACHE) page_id = page_of(j + brings * 16);
     };
     // The last columns of a prompt end a tile, not begin one: what would lie past them is taken from before, where the tile before has it
     // already (and these are hidden).  Keys of the tile whose first key would be j begin at:
@@ -703,7 +797,7 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
     // the tile whose keys are j and up; next: those of the tile after it
     const auto load_begin = [&](int j, int next) __attribute__((always_inline)) {
         if constexpr (CACHE) {
-            const int at = (j + brings * 16) & (page - 1);     // a wavefront brings 16 keys (and their values)
+            const int at = ((j >= lift ? j - lift : j) + brings * 16) & (page - 1);     // a wavefront brings 16 keys (and their values)
             known = (unsigned)page_id < (unsigned)a.pages;
             const char* base = pages + (known ? page_id : 0) * page_bytes;
 #pragma unroll
@@ -838,7 +932,7 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
             }
             if (is_masked(j) || (!CACHE && j < hide))
                 attn_hide<16>(
-                    j + (CACHE ? 4 : 8) * half, p, lo, CACHE ? 0 : hide, a.sinks, j < a.sinks,
+                    j + (CACHE ? 4 : 8) * half, p, lo, CACHE ? 0 : hide, sinks, j < sinks,
                     [](int i) __attribute__((always_inline)) { return CACHE ? 8 * (i >> 2) + (i & 3) : 16 * (i >> 3) + (i & 7); },
                     [&](int i) __attribute__((always_inline)) { sc[SUB][i] = -INFINITY; });
         }
@@ -965,11 +1059,11 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
             const int from_key = first_key(v);
             if (!partial(from_key)) continue;
             for (int k = from_key; k < from_key + ATTN_TILE_KEYS; ++k) {
-                if (!attn_sees(k, p, lo, a.sinks)) continue;
+                if (!attn_sees(k, p, lo, sinks)) continue;
                 if constexpr (CACHE) {
-                    const int id = a.table[(int64_t)b * a.table_ld + (k >> a.page_shift)];
+                    const int id = page_of(k), at = (k >= lift ? k - lift : k) & (page - 1);
                     const bool there = (unsigned)id < (unsigned)a.pages;
-                    const char* sc8 = pages + (there ? id : 0) * page_bytes + (int64_t)page * D + (int64_t)(page + (k & (page - 1))) * SB;
+                    const char* sc8 = pages + (there ? id : 0) * page_bytes + (int64_t)page * D + (int64_t)(page + at) * SB;
 #pragma unroll
                     for (int t = 0; t < DT; ++t)
                         if (!there || (unsigned char)sc8[t] > most_scale(BF)) o[t] += __builtin_nanf("");
@@ -988,7 +1082,9 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
 
     const float2v both = attn_pair32(l);
     l = both[0] + both[1];
-    if (!works || query >= seq.nq) return;
+    const Column own_column = column();
+    const int head = own_column.head, query = own_column.query;
+    if (!works || !own_column.real) return;
     if (seq.bad) l = __builtin_nanf("");
     const int64_t token = seq.t0 + query;
     if (!a.part_o) {
@@ -1025,7 +1121,7 @@ __global__ __launch_bounds__(FEW ? 256 : 1024) void attention_join_kernel(AttnAr
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t token0 = (int64_t)blockIdx.x * TOKENS;
     int64_t begin = 0, end = a.tokens;
-    if (a.shared && a.starts) {                            // columns of no sequence have no parts
+    if ((a.shared || a.behind) && a.starts) {              // columns of no sequence have no parts
         begin = a.starts[0];
         end = a.starts[a.sequences] < end ? a.starts[a.sequences] : end;
     }

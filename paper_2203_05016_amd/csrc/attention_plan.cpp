@@ -24,6 +24,55 @@ int64_t keys_seen(int64_t max_length, int window, int sinks, int64_t queries)
     return std::min<int64_t>(max_length, (int64_t)window + sinks + queries);
 }
 
+// The keys' cut into parts: of `base` workgroups, `slots` of which the GPU holds, each part worth `least` tiles or more
+void cut(AttnPlan& p, int64_t base, int64_t slots, int64_t least, int64_t tiles)
+{
+    // One cut for all sequences, by max_length.  Where that is the table's capacity, parts past a sequence's keys have no work: one of 30000 keys, 64
+    // heads over 8 of 128, 16.3 us cut by its length and 24.6 by a table of 131072; 16 of 3000 on average 20.1 and 30.7 by one of 32768.
+    // Keys are cut into parts where workgroups are few, into as many as fill the GPU once (what is left over costs a whole round: 24
+    // sequences of 3000 keys, 8 heads of 128, 5 queries of 64 heads 48 us in 3 parts of 4 wavefronts, 41 in 2).  The join takes 4
+    // to 5 us, so parts are not worth it under twice their least length.
+    int64_t splits = base > 0 && tiles >= 2 * least ? std::min(slots / base, tiles / least) : 1;
+    splits = std::max<int64_t>(splits, 1);
+    p.split_tiles = (int)ceil_div(tiles, splits);
+    p.splits = (int)ceil_div(tiles, p.split_tiles);
+    p.groups = product(base, p.splits);
+}
+
+// The tile kernel over the cache, for `items` of each of `pairs`, that see up to `keys`
+AttnPlan plan_tiles(int64_t pairs, int64_t items, int D, int64_t keys)
+{
+    AttnPlan p = {};
+    // 8 wavefronts share what they bring; 4 where there are no more items (4 sequences of up to 9000 keys, 1024 queries, 32 heads over 8 of
+    // 96 410 us with 8, 428 with 4)
+    p.waves = items > 4 ? 8 : 4;
+    const int64_t col_blocks = ceil_div(items, p.waves);
+    // (parts of 4 tiles: 633 queries of 1 sequence of 1222 keys, 4 heads of 128: 25 us in parts of 4 tiles, 31 of 8)
+    cut(p, product(pairs, col_blocks), p.waves == 4 && D < 128 ? 2 * CUS : CUS /* what the LDS holds of three tiles */, 4, keys / ATTN_TILE_KEYS + 3);
+    p.col_blocks = (int)std::min<int64_t>(col_blocks, INT32_MAX);   // (more are more groups than a launch takes)
+    return p;
+}
+
+// The prefixes' part: max_sharing queries of each of `pairs`, all of which see all `keys`.  Up to 192 columns by the kernel for few queries in blocks of 32
+// (64 heads over 8 of 128, one prefix of 8000: 24 sequences 30.4 us, in tiles of queries 37.6; 16 prefixes of 3000 with 24 each 99 and 100), up to 256
+// while the GPU holds the blocks (32: 30.3 and 40.7; 16 prefixes with 32 each 132 and 108); blocks of 48 where these are fewer by a fourth and the GPU is
+// full (16 prefixes with 12 sequences each 59 us, in blocks of 32 66; with 16 81 and 71; one prefix with 12 30.0 and 25.7).
+AttnPlan plan_prefix(int64_t pairs, int group, int D, int64_t max_sharing, int64_t keys)
+{
+    AttnPlan p = {};
+    const int64_t columns = product(max_sharing, group);
+    const int64_t twos = ceil_div(columns, 32), threes = ceil_div(columns, 48);
+    if (group > 32 || columns > 256 || (columns > 192 && product(pairs, twos) > CUS)) return plan_tiles(pairs, ceil_div(columns, ATTN_TILE_QUERIES), D, keys);
+    p.decode = true;
+    p.col_tiles = columns <= 16 ? 1 : pairs * twos >= CUS && 4 * threes < 3 * twos ? 3 : 2;
+    const int64_t col_blocks = ceil_div(max_sharing, 16 * p.col_tiles / group);
+    const int residency = decode_residency(p.col_tiles, D);
+    p.waves = residency > 1 && pairs * col_blocks <= CUS * (residency / 2) ? 8 : 4;
+    cut(p, product(pairs, col_blocks), p.waves == 8 ? CUS * (residency / 2) : CUS * residency, 4 * p.waves, keys / ATTN_DECODE_KEYS + 3);
+    p.col_blocks = (int)col_blocks;
+    return p;
+}
+
 }  // namespace
 
 AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t tokens, int max_queries, int64_t max_length, int window, int sinks)
@@ -39,7 +88,8 @@ AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t to
     const bool cuts = group <= 32;                 // blocks are of whole queries
     const int64_t blocks_of_32 = cuts ? ceil_div(max_queries, 32 / group) : 1;
     p.decode = columns <= 64 || (cuts && columns <= 128 && pairs * blocks_of_32 <= 2 * CUS);
-    int64_t slots, least;   // workgroups the GPU holds at a time, and tiles that a part is worth
+    // keys that the queries of one workgroup see: window and sinks each may begin inside a tile
+    const int64_t keys = keys_seen(max_length, window, sinks, max_queries);
     if (p.decode) {
         p.col_tiles = (int)ceil_div(columns, 16);
         // 64 columns leave one wavefront per SIMD (D = 128): two blocks of 32, of whole queries, read the cache twice and are faster.  16
@@ -53,43 +103,39 @@ AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t to
         // of 128: 40 us with 8, 44 with 4; 128 of 1028, 16 heads of 64: 35 and 29.
         const int residency = decode_residency(p.col_tiles, D);
         p.waves = residency > 1 && pairs * col_blocks <= CUS * (residency / 2) ? 8 : 4;
-        slots = p.waves == 8 ? CUS * (residency / 2) : CUS * residency;
-        least = 4 * p.waves;
+        const int64_t slots = p.waves == 8 ? CUS * (residency / 2) : CUS * residency;
+        cut(p, product(pairs, col_blocks), slots, 4 * p.waves, keys / ATTN_DECODE_KEYS + 3);
+        p.col_blocks = (int)std::min<int64_t>(col_blocks, INT32_MAX);
     } else {
-        const int64_t items = ceil_div(max_queries, ATTN_TILE_QUERIES) * group;
-        // 8 wavefronts share what they bring; 4 where there are no more items (4 sequences of up to 9000 keys, 1024 queries, 32 heads over 8 of
-        // 96 410 us with 8, 428 with 4)
-        p.waves = items > 4 ? 8 : 4;
-        col_blocks = ceil_div(items, p.waves);
-        slots = p.waves == 4 && D < 128 ? 2 * CUS : CUS;   // what the LDS holds of three tiles
-        least = 4;   // 633 queries of 1 sequence of 1222 keys, 4 heads of 128: 25 us in parts of 4 tiles, 31 of 8
+        p = plan_tiles(pairs, ceil_div(max_queries, ATTN_TILE_QUERIES) * group, D, keys);
     }
-    const int tile = p.decode ? ATTN_DECODE_KEYS : ATTN_TILE_KEYS;
-    const int64_t base = product(pairs, col_blocks);
-    // tiles of the longest sequence: window and sinks each may begin inside a tile
-    const int64_t tiles = keys_seen(max_length, window, sinks, max_queries) / tile + 3;
-    // One cut for all sequences, by max_length.  Where that is the table's capacity, parts past a sequence's keys have no work: one of 30000 keys, 64
-    // heads over 8 of 128, 16.3 us cut by its length and 24.6 by a table of 131072; 16 of 3000 on average 20.1 and 30.7 by one of 32768.
-    // Keys are cut into parts where workgroups are few, into as many as fill the GPU once (what is left over costs a whole round: 24
-    // sequences of 3000 keys, 8 heads of 128, 5 queries of 64 heads 48 us in 3 parts of 4 wavefronts, 41 in 2).  The join takes 4
-    // to 5 us, so parts are not worth it under twice their least length.
-    int64_t splits = base > 0 && tiles >= 2 * least ? std::min(slots / base, tiles / least) : 1;
-    splits = std::max<int64_t>(splits, 1);
-    p.split_tiles = (int)ceil_div(tiles, splits);
-    p.splits = (int)ceil_div(tiles, p.split_tiles);
-    p.groups = product(base, p.splits);
-    p.col_blocks = (int)std::min<int64_t>(col_blocks, INT32_MAX);   // (more are more groups than a launch takes)
     p.workspace = p.splits > 1 ? (int64_t)p.splits * heads * group * tokens * (D + 2) * 4 : 0;
     return p;
 }
 
 SharedPlan plan_shared_attention(int prefixes, int64_t max_sharing, int64_t max_prefix, int batch, int heads, int group, int D, int64_t tokens, int max_queries,
-                                 int64_t max_length)
+                                 int64_t max_length, bool keys_fit)
 {
     SharedPlan p = {};
-    p.prefix = plan_cache_attention(prefixes, heads, group, D, tokens, (int)std::min<int64_t>(max_sharing, INT32_MAX), max_prefix, INT32_MAX, 0);
+    max_queries = (int)std::max<int64_t>(1, std::min<int64_t>(max_queries, tokens));
+    max_sharing = std::max<int64_t>(1, std::min<int64_t>(max_sharing, tokens));
+    const auto parts = [&](int64_t n) { return product(n * (D + 2) * 4, (int64_t)heads * group * tokens); };
+    // From 20 queries on, sequence by sequence: a prefix's parts, in 32 bits, are then more than its keys.  32 sequences behind 4096 tokens, 64 heads over 8 of
+    // 128: 16 queries 137 us, prefix and own apart 116; 20 131 and 151, 32 129 and 180, 33 240 and 292; 8 of 512 504 and 752.
+    p.behind = keys_fit && max_queries >= 20;
+    if (p.behind) {
+        p.own = plan_tiles((int64_t)batch * heads, ceil_div(max_queries, ATTN_TILE_QUERIES) * group, D, max_prefix + ATTN_TILE_KEYS + max_length);
+        p.workspace = p.own.splits > 1 ? parts(p.own.splits) : 0;
+        return p;
+    }
+    p.prefix = plan_prefix((int64_t)prefixes * heads, group, D, max_sharing, max_prefix);
     p.own = plan_cache_attention(batch, heads, group, D, tokens, max_queries, max_length, INT32_MAX, 0);
-    p.workspace = product((int64_t)(p.prefix.splits + p.own.splits) * (D + 2) * 4, (int64_t)heads * group * tokens);
+    // The kernel for few queries joins the prefixes' parts with what it finds, if there are no parts of its own keys, and if what a workgroup then
+    // fetches is little: 64 sequences, 64 heads over 8 of 128, 16 parts 46 us, by a kernel of its own 54; 8 with 32 parts 26 and 25; 8 queries of each of
+    // 64, 8 parts, 125 and 115.
+    const int64_t fetched = (int64_t)std::min(16 * p.own.col_tiles, group * max_queries) * p.prefix.splits * D * 4;
+    p.joins = p.own.decode && p.own.splits == 1 && p.prefix.splits <= ATTN_JOINED && fetched <= (p.own.groups >= CUS ? 65536 : 16384);
+    p.workspace = parts((int64_t)p.prefix.splits + (p.joins ? 0 : p.own.splits));
     return p;
 }
 
