@@ -187,8 +187,8 @@ int shflbw_kv_shared_attention(const shflbw_kv_cache* cache, const shflbw_kv_pre
             own.part_o = static_cast<float*>(workspace);
             own.part_ml = own.part_o + parts * rows * cache->head_dim;
         }
-        return cache->dtype == SHFLBW_BF16 ? run_attention_bf16(own, plan.own, cache->head_dim, false, stream)
-                                           : run_attention_f16(own, plan.own, cache->head_dim, false, stream);
+        return cache->dtype == SHFLBW_BF16 ? run_shared_attention_bf16(own, own, plan, cache->head_dim, stream)
+                                           : run_shared_attention_f16(own, own, plan, cache->head_dim, stream);
     }
     AttnArgs prefix = cache_args(cache, s, plan.prefix, q, ldq);
     prefix.table = prefixes->table;

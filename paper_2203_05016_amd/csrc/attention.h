@@ -64,7 +64,7 @@ struct AttnArgs {
     bool shared;
     const int32_t* members;
     int sequences;            // of `starts`
-    // Sequences behind prefixes (the tile kernel): their keys are the prefix's, from 0 on, and their own, from the next multiple of a tile on
+    // Sequences behind prefixes: their keys are the prefix's, from 0 on, and their own, from the next multiple of a tile on
     bool behind;
     const int32_t *prefix_table, *prefix_lengths;
     int64_t prefix_ld;

@@ -118,18 +118,26 @@ __device__ __forceinline__ attn_table attn_scalar(const int32_t* p) { return (at
 // The row among parts' of a column whose head is in the upper and whose token in the lower 32 bits
 __device__ __forceinline__ int64_t attn_row(const AttnArgs& a, int64_t where) { return (where >> 32) * a.tokens + (where & 0xffffffffLL); }
 
+// Whether a call has prefixes.  Its kernels are their own: what the others would carry along costs one query of one sequence 7 % (7.3 us, 7.9), a batch 2 %.
+struct AttnPlainCall {
+    static constexpr bool SHARED = false;
+};
+struct AttnSharedCall {
+    static constexpr bool SHARED = true;
+};
+
 // One sequence of a call
 struct AttnSeq {
     int64_t t0;    // its first column of q
     int nq, len;   // queries, and keys up to the last query's own
     bool bad;      // longer than its pages can be
 };
-template <bool CACHE>
+template <bool CACHE, bool SHARED = false>
 __device__ __forceinline__ AttnSeq attn_sequence(const AttnArgs& a, int b)
 {
     AttnSeq s;
     int64_t t0 = CACHE ? b : 0, t1 = CACHE ? b + 1 : a.tokens;
-    if (CACHE && a.shared) {
+    if (SHARED && a.shared) {
         t0 = a.members ? attn_scalar(a.members)[b] : 0;
         t1 = a.members ? attn_scalar(a.members)[b + 1] : a.sequences;
         t0 = t0 < 0 ? 0 : t0 > a.sequences ? a.sequences : t0;
@@ -170,6 +178,24 @@ __device__ __forceinline__ int attn_prefix_of(const AttnArgs& a, int b)
         else high = mid;
     }
     return members[low] <= b && b < members[low + 1] ? low : -1;
+}
+
+// What a sequence has behind its prefix: keys from `lift` on, a multiple of `tile`, are its own; the first `sinks` are the prefix's, which all queries see
+struct AttnBehind {
+    int lift, sinks;
+    attn_table table;
+};
+template <bool SHARED>
+__device__ __forceinline__ AttnBehind attn_behind(const AttnArgs& a, AttnSeq& seq, int b, int tile)
+{
+    if (!SHARED || !a.behind) return AttnBehind{0, a.sinks, nullptr};
+    const int g = attn_prefix_of(a, b), most = a.prefix_width << a.page_shift, length = g < 0 ? 0 : attn_scalar(a.prefix_lengths)[g];
+    seq.bad |= length > most;
+    AttnBehind r;
+    r.sinks = length > most ? most : length < 0 ? 0 : length;
+    r.lift = (r.sinks + tile - 1) / tile * tile;
+    r.table = attn_scalar(a.prefix_table + (g < 0 ? 0 : g) * a.prefix_ld);
+    return r;
 }
 
 // The tiles of keys (shifted by `shift`: tile t holds keys tile * t - shift and up) that queries at positions first..last need: those of
@@ -222,9 +248,10 @@ __device__ __forceinline__ float attn_max3(float a, float b, float c) { return f
 // 2 of 131071 keys (f16, 277 MB) 48 us, 5.8 TB/s (part of it lies in the memory-side cache), and 4.2 for the join; 128 under a window of
 // 1024 with 4 sinks, 16 heads of 64, 144 MB: 30 us, 4.7 TB/s.  Vector instructions are issued in 32 % of the cycles, the matrix units busy in 10.
 // With 5 queries each (48 columns; 24 sequences of up to 3001 keys, 56 MB) 34 us: a CU has 8 wavefronts, half of the CUs none.
-template <bool BF, int D, int NT, int W>
+template <bool BF, int D, int NT, int W, class CALL>
 __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_decode_kernel(AttnArgs a)
 {
+    constexpr bool SHARED = CALL::SHARED;
     constexpr int S = D / 32, DT = D / 16, C = 16 * NT;
     constexpr int VP = 2 * D + 32;                        // LDS pitch of a key's values: 8 rows x 32 bytes in 64 banks
     constexpr int OP = D + 4;                             // pitch of a column's sums, in floats
@@ -247,13 +274,19 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
     const int b = pair / a.heads, h = pair % a.heads;
 
     // a block of columns is a whole number of queries
-    AttnSeq seq = attn_sequence<true>(a, b);
+    AttnSeq seq = attn_sequence<true, SHARED>(a, b);
     const int skipped = block * (C / a.group), left = seq.nq - skipped;
     if (left <= 0) return;
     const int cols = (left < C / a.group ? left : C / a.group) * a.group;
     seq.t0 += skipped;
-    const int p_first = a.shared ? seq.len - 1 : seq.len - left, p_last = a.shared ? p_first : p_first + (cols - 1) / a.group;
-    const AttnTiles tiles = attn_tiles(p_first, p_last, a.window, a.sinks, 0, ATTN_DECODE_KEYS);
+    const AttnBehind prefix = attn_behind<SHARED>(a, seq, b, ATTN_DECODE_KEYS);
+    const int lift = prefix.lift, sinks = prefix.sinks;
+    // (before all own keys: the prefix alone, or nothing)
+    const bool flat = SHARED && a.shared, behind = SHARED && a.behind, joined = SHARED && a.joined;
+    const int p0 = flat ? seq.len - 1 : lift + seq.len - left, advance = flat ? 0 : 1;
+    const auto position = [&](int query) __attribute__((always_inline)) { return SHARED ? max(p0 + advance * query, lift - 1) : p0 + query; };
+    const int p_first = position(0), p_last = position((cols - 1) / a.group);
+    const AttnTiles tiles = attn_tiles(p_first, p_last, a.window, behind ? 0 : sinks, 0, ATTN_DECODE_KEYS);
     const int v_begin = split * a.split_tiles;
     // the last part takes what is left, also of a sequence longer than the plan was told
     const int v_end = split + 1 == a.splits || tiles.count - v_begin < a.split_tiles ? tiles.count : v_begin + a.split_tiles;
@@ -270,11 +303,12 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
     };
     // page of tile v; tiles past the end read what the last one does
     const auto page_of = [&](int v) __attribute__((always_inline)) {
-        return table[tiles.real(v < v_end ? v : v_end - 1) * ATTN_DECODE_KEYS >> a.page_shift];
+        const int j = tiles.real(v < v_end ? v : v_end - 1) * ATTN_DECODE_KEYS;
+        return SHARED && j < lift ? prefix.table[j >> a.page_shift] : table[j - lift >> a.page_shift];
     };
     const auto load = [&](Raw& x, int v, int id) __attribute__((always_inline)) {
         const bool known = (unsigned)id < (unsigned)a.pages;
-        const int at = tiles.real(v < v_end ? v : v_end - 1) * ATTN_DECODE_KEYS & (page - 1);
+        const int j = tiles.real(v < v_end ? v : v_end - 1) * ATTN_DECODE_KEYS, at = (SHARED && j < lift ? j : j - lift) & (page - 1);
         const char* base = pages + (known ? id : 0) * page_bytes;
         const char* codes = base + code_offset(D, at, 0);
         const unsigned code_lane = D == 64 ? lane * 16 : lane * (D / 8);
@@ -329,7 +363,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
 #pragma unroll
             for (int k = 0; k < D / (W * FS); ++k) *reinterpret_cast<uint16_t*>(smem + c * QP + (f0 + k * W * FS) * 2) = real ? x[k] : 0;
         // where a column's results go: head and token
-        if (wave == 0 && n < C) where[c] = a.joined ? (int64_t)(h * a.group + g) << 32 | (seq.t0 + i) : !a.part_o ? (int64_t)(h * a.group + g) * D * a.ldo + seq.t0 + i
+        if (wave == 0 && n < C) where[c] = joined ? (int64_t)(h * a.group + g) << 32 | (seq.t0 + i) : !a.part_o ? (int64_t)(h * a.group + g) * D * a.ldo + seq.t0 + i
                                                          : ((int64_t)split * a.heads * a.group + h * a.group + g) * a.tokens + seq.t0 + i;
         __syncthreads();
 #pragma unroll
@@ -340,8 +374,8 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int col = 16 * n + r;
-            p[n] = col < cols ? p_first + (a.shared ? 0 : col / a.group) : -1;
-            lo[n] = attn_window_start(p[n], a.window);
+            p[n] = col < cols ? position(col / a.group) : -1;
+            lo[n] = behind ? lift : attn_window_start(p[n], a.window);
         }
     }
 
@@ -353,11 +387,11 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
     char* vt = smem + wave * 32 * VP;
     char* vw = vt + v_row * VP + v_part * 16;
     const attn_lds vr = (attn_lds)vt + (4 * quarter + (r >> 2)) * VP + (r & 3) * 8;
-    const int window_last = attn_window_start(p_last, a.window);
+    const int window_last = behind ? lift : attn_window_start(p_last, a.window);
 
     bool special = false;
     // whether not all columns see all 32 keys from j on
-    const auto is_masked = [&](int j) __attribute__((always_inline)) { return j + 31 > p_first || (j < window_last && j + 31 >= a.sinks); };
+    const auto is_masked = [&](int j) __attribute__((always_inline)) { return j + 31 > p_first || (j < window_last && j + 31 >= sinks); };
     const auto work = [&](Raw& raw, int v) __attribute__((always_inline)) {
         const int j0 = tiles.real(v) * ATTN_DECODE_KEYS;
         if (!raw.known)                                   // a page that is not there reads as NaN
@@ -399,7 +433,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (!attn_sees(j0 + (i >> 2) * 16 + quarter * 4 + (i & 3), p[n], lo[n], a.sinks)) sc[n][i >> 2][i & 3] = -INFINITY;
+                    if (!attn_sees(j0 + (i >> 2) * 16 + quarter * 4 + (i & 3), p[n], lo[n], sinks)) sc[n][i >> 2][i & 3] = -INFINITY;
         float top[NT];
         bool grown = false;
 #pragma unroll
@@ -451,12 +485,12 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
             const int j0 = tiles.real(v) * ATTN_DECODE_KEYS;
             if (!is_masked(j0)) continue;
             for (int j = j0; j < j0 + ATTN_DECODE_KEYS && j <= p_last; ++j) {
-                const int page_j = table[j >> a.page_shift];
+                const int k = SHARED && j < lift ? j : j - lift, page_j = (SHARED && j < lift ? prefix.table : table)[k >> a.page_shift];
                 const bool there = (unsigned)page_j < (unsigned)a.pages;
-                const char* scales = pages + (there ? page_j : 0) * page_bytes + (int64_t)page * D + (int64_t)(page + (j & (page - 1))) * SB;
+                const char* scales = pages + (there ? page_j : 0) * page_bytes + (int64_t)page * D + (int64_t)(page + (k & (page - 1))) * SB;
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
-                    if (attn_sees(j, p[n], lo[n], a.sinks))
+                    if (attn_sees(j, p[n], lo[n], sinks))
 #pragma unroll
                         for (int t = 0; t < DT; ++t)
                             if (!there || (unsigned char)scales[t / 2] > most_scale(BF)) o[n][t] += __builtin_nanf("");
@@ -487,7 +521,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
         for (int i = 0; i < W; ++i) total += stat[i][col][1] * attn_exp2(stat[i][col][0] - top);
         if (seq.bad) total = __builtin_nanf("");
         float f = attn_exp2(m[n] - top);
-        if (a.joined) {
+        if (joined) {
             if (wave == 0 && quarter == 0) {
                 own[2 * r] = p[n] < 0 ? -INFINITY : top;
                 own[2 * r + 1] = total;
@@ -502,7 +536,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
 #pragma unroll
         for (int t = 0; t < DT; ++t) *reinterpret_cast<float4v*>(sums + (wave * 16 + r) * OP + 16 * t + 4 * quarter) = o[n][t] * f;
         __syncthreads();
-        if (a.joined) {
+        if (joined) {
             // 32 lanes to a column, one to a part
             for (int c = threadIdx.x >> 5; c < 16 && 16 * n + c < cols; c += 2 * W) {
                 const int part = threadIdx.x & 31;
@@ -531,7 +565,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
             float x = 0;
 #pragma unroll
             for (int i = 0; i < W; ++i) x += sums[(i * 16 + c) * OP + d];
-            if (a.joined) {
+            if (joined) {
                 const float* w = weight + c * (ATTN_JOINED + 1);
                 const float* from = a.joined_o + attn_row(a, where[at]) * D + d;
                 const int64_t step = (int64_t)a.heads * a.group * a.tokens * D;
@@ -539,7 +573,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
 #pragma unroll 8
                 for (int i = 0; i < a.joined; ++i, from += step) x += *from * w[i];
             }
-            if (a.joined) a.out[((where[at] >> 32) * D + d) * a.ldo + (where[at] & 0xffffffffLL)] = attn_narrow<BF>(x);
+            if (joined) a.out[((where[at] >> 32) * D + d) * a.ldo + (where[at] & 0xffffffffLL)] = attn_narrow<BF>(x);
             else if (!a.part_o) a.out[where[at] + d * a.ldo] = attn_narrow<BF>(x);
             else a.part_o[where[at] * D + d] = x;
         }
@@ -653,10 +687,11 @@ __device__ __forceinline__ void attn_infinite_sums(float16v (&o)[D / 32], const 
 }
 
 // TINY: a prompt of fewer than 64 columns in all.
-template <bool BF, int D, bool CACHE, int W, bool TINY = false>
+template <bool BF, int D, bool CACHE, int W, bool TINY, class CALL>
 __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention_tile_kernel(AttnArgs a)
 {
     using Stage = AttnStage<BF, D, CACHE>;
+    constexpr bool SHARED = CALL::SHARED;
     constexpr int S = D / 16, DT = D / 32, KP = Stage::KP, VP = Stage::VP;
     constexpr int SB = scale_bytes(D);
     constexpr int KINDS = W == 8 ? 1 : 2;                  // four wavefronts bring keys and values, of eight each four one of them
@@ -672,36 +707,27 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
     const int blk = a.col_blocks - 1 - inner / a.splits, split = inner % a.splits;
     const int b = pair / a.heads, h = pair % a.heads;
 
-    AttnSeq seq = attn_sequence<CACHE>(a, b);
+    AttnSeq seq = attn_sequence<CACHE, SHARED>(a, b);
     // A prefix's queries are taken as they come, 32 columns of all of the group's heads at a time: all see the same keys
-    const bool flat = CACHE && a.shared;
+    const bool flat = SHARED && a.shared, behind = SHARED && a.behind;
     const int64_t columns = (int64_t)seq.nq * a.group;
     const int64_t items = flat ? (columns + ATTN_TILE_QUERIES - 1) / ATTN_TILE_QUERIES : (int64_t)((seq.nq + ATTN_TILE_QUERIES - 1) / ATTN_TILE_QUERIES) * a.group;
     const int64_t item0 = (int64_t)blk * W;
     if (item0 >= items) return;
     const int64_t item_last = items < item0 + W ? items - 1 : item0 + W - 1;
     const int shift = CACHE ? 0 : (int)(seq.t0 & 7);       // tiles of a prompt begin at multiples of 8 columns
-    // Behind a prefix the own keys begin at `lift`, and the first `sinks` keys, the prefix's, are seen by all
-    int lift = 0, sinks = a.sinks;
-    attn_table prefix_table = nullptr;
-    if (CACHE && a.behind) {
-        const int g = attn_prefix_of(a, b), most = a.prefix_width << a.page_shift;
-        const int length = g < 0 ? 0 : attn_scalar(a.prefix_lengths)[g];
-        seq.bad |= length > most;
-        sinks = length > most ? most : length < 0 ? 0 : length;
-        lift = (sinks + ATTN_TILE_KEYS - 1) / ATTN_TILE_KEYS * ATTN_TILE_KEYS;
-        prefix_table = attn_scalar(a.prefix_table + (g < 0 ? 0 : g) * a.prefix_ld);
-    }
+    const AttnBehind prefix = attn_behind<SHARED>(a, seq, b, ATTN_TILE_KEYS);
+    const int lift = prefix.lift, sinks = prefix.sinks;
     const int p0 = lift + seq.len - seq.nq;
     const auto position = [&](int64_t query) {
         if (flat) return seq.len - 1;
         const int at = p0 + (int)(query < seq.nq ? query : seq.nq - 1);
-        return CACHE && at < lift ? lift - 1 : at;         // (before all own keys: the prefix alone, or nothing)
+        return SHARED && at < lift ? lift - 1 : at;         // (before all own keys: the prefix alone, or nothing)
     };
-    const auto window_start = [&](int p) { return CACHE && a.behind ? lift : attn_window_start(p, a.window); };
+    const auto window_start = [&](int p) { return behind ? lift : attn_window_start(p, a.window); };
     const int wg_first = position(item0 / a.group * ATTN_TILE_QUERIES);
     const int wg_last = position(item_last / a.group * ATTN_TILE_QUERIES + ATTN_TILE_QUERIES - 1);
-    const AttnTiles tiles = attn_tiles(wg_first, wg_last, a.window, CACHE && a.behind ? 0 : sinks, shift, ATTN_TILE_KEYS);
+    const AttnTiles tiles = attn_tiles(wg_first, wg_last, a.window, behind ? 0 : sinks, shift, ATTN_TILE_KEYS);
     const int v_begin = split * (a.splits > 1 ? a.split_tiles : 0);
     const int v_end = split + 1 == a.splits || tiles.count - v_begin < a.split_tiles ? tiles.count : v_begin + a.split_tiles;   // (as in the other kernel)
 
@@ -783,9 +809,9 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
     }
     // a tile's keys are all the prefix's or all the sequence's own; keys past the last page are hidden
     const auto page_of = [&](int j) __attribute__((always_inline)) {
-        const bool own = j >= lift;
+        const bool own = !SHARED || j >= lift;
         const int idx = (own ? j - lift : j) >> a.page_shift, width = own ? a.table_width : a.prefix_width;
-        return (own ? table : prefix_table)[idx < width ? idx : width - 1];
+        return (own ? table : prefix.table)[idx < width ? idx : width - 1];
     };
     const auto find_page = [&](int j) __attribute__((always_inline)) {
         if constexpr (CACHE) page_id = page_of(j + brings * 16);
@@ -797,7 +823,7 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
     // the tile whose keys are j and up; next: those of the tile after it
     const auto load_begin = [&](int j, int next) __attribute__((always_inline)) {
         if constexpr (CACHE) {
-            const int at = ((j >= lift ? j - lift : j) + brings * 16) & (page - 1);     // a wavefront brings 16 keys (and their values)
+            const int at = ((!SHARED || j >= lift ? j - lift : j) + brings * 16) & (page - 1);     // a wavefront brings 16 keys (and their values)
             known = (unsigned)page_id < (unsigned)a.pages;
             const char* base = pages + (known ? page_id : 0) * page_bytes;
 #pragma unroll
@@ -1061,7 +1087,7 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
             for (int k = from_key; k < from_key + ATTN_TILE_KEYS; ++k) {
                 if (!attn_sees(k, p, lo, sinks)) continue;
                 if constexpr (CACHE) {
-                    const int id = page_of(k), at = (k >= lift ? k - lift : k) & (page - 1);
+                    const int id = page_of(k), at = (!SHARED || k >= lift ? k - lift : k) & (page - 1);
                     const bool there = (unsigned)id < (unsigned)a.pages;
                     const char* sc8 = pages + (there ? id : 0) * page_bytes + (int64_t)page * D + (int64_t)(page + at) * SB;
 #pragma unroll
@@ -1113,7 +1139,7 @@ __global__ __launch_bounds__(64 * W, tile_residency(D, CACHE, W)) void attention
 // A wavefront takes one token of one query head, its lanes two features each, and reads the parts' sums along the features, all of
 // them at once; a workgroup's results leave along the tokens.  Where there are few rows, the parts of a row are shared by the
 // workgroup's four wavefronts instead.  Bound by latency where it matters: 128 rows of 32 parts 4.2 us.
-template <bool BF, int D, bool FEW>
+template <bool BF, int D, bool FEW, class CALL>
 __global__ __launch_bounds__(FEW ? 256 : 1024) void attention_join_kernel(AttnArgs a)
 {
     constexpr int TOKENS = FEW ? 1 : 16;
@@ -1121,7 +1147,7 @@ __global__ __launch_bounds__(FEW ? 256 : 1024) void attention_join_kernel(AttnAr
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t token0 = (int64_t)blockIdx.x * TOKENS;
     int64_t begin = 0, end = a.tokens;
-    if ((a.shared || a.behind) && a.starts) {              // columns of no sequence have no parts
+    if (CALL::SHARED && a.starts) {                        // columns of no sequence have no parts
         begin = a.starts[0];
         end = a.starts[a.sequences] < end ? a.starts[a.sequences] : end;
     }

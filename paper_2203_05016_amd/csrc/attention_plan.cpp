@@ -122,9 +122,16 @@ SharedPlan plan_shared_attention(int prefixes, int64_t max_sharing, int64_t max_
     const auto parts = [&](int64_t n) { return product(n * (D + 2) * 4, (int64_t)heads * group * tokens); };
     // From 20 queries on, sequence by sequence: a prefix's parts, in 32 bits, are then more than its keys.  32 sequences behind 4096 tokens, 64 heads over 8 of
     // 128: 16 queries 137 us, prefix and own apart 116; 20 131 and 151, 32 129 and 180, 33 240 and 292; 8 of 512 504 and 752.
-    p.behind = keys_fit && max_queries >= 20;
+    // And few queries where reading the prefix again for every sequence, from the L2s, is less than parts and another launch: up to 2^27 values (bytes, as
+    // the cache has them, are 17/32 of that).  64 heads over 8 of 128: 8 sequences behind 500 tokens 8.5 us and 18.8 apart, 32 behind 1000 12.0 and 22.7, behind 2000
+    // (131 million) 20.7 and 23.6; 32 over 8 of 96, 8 prefixes of 3000 with 4 each (147 million) 20.2 and 18.0.
+    const bool many = max_queries >= 20;
+    const int64_t again = product((int64_t)batch * heads * 2 * D, max_prefix);
+    p.behind = keys_fit && (many || ((int64_t)group * max_queries <= 64 && again <= 1LL << 27));
     if (p.behind) {
-        p.own = plan_tiles((int64_t)batch * heads, ceil_div(max_queries, ATTN_TILE_QUERIES) * group, D, max_prefix + ATTN_TILE_KEYS + max_length);
+        const int64_t keys = max_prefix + ATTN_TILE_KEYS + max_length;
+        p.own = many ? plan_tiles((int64_t)batch * heads, ceil_div(max_queries, ATTN_TILE_QUERIES) * group, D, keys)
+                     : plan_cache_attention(batch, heads, group, D, tokens, max_queries, keys, INT32_MAX, 0);
         p.workspace = p.own.splits > 1 ? parts(p.own.splits) : 0;
         return p;
     }

@@ -1,5 +1,4 @@
 // Attention launchers for bfloat16 operands.
 #define SHFLBW_LAUNCH_BF true
 #define SHFLBW_LAUNCH_NAME run_attention_bf16
-#define SHFLBW_LAUNCH_SHARED run_shared_attention_bf16
 #include "launch_attention.inc"

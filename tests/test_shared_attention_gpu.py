@@ -27,9 +27,10 @@ def _int(values):
 
 class Served:
     """Prefixes, and sequences' own tokens, in one cache whose pages lie in no order and whose other slots read as NaN.  families: how
-    many sequences every prefix has."""
+    many sequences every prefix has.  apart: the prefixes' table has room for so many pages that prefix and own tokens are attended to by kernels of their
+    own, unless the host says that prefixes are short."""
 
-    def __init__(self, prefixes, families, own, heads, D, page, dtype, seed=0, spare=1):
+    def __init__(self, prefixes, families, own, heads, D, page, dtype, seed=0, apart=False):
         self.heads, self.D, self.page, self.dtype = heads, D, page, dtype
         self.prefixes, self.own = prefixes, own
         self.family = [g for g, n in enumerate(families) for _ in range(n)]
@@ -47,8 +48,9 @@ class Served:
             k, v = _tensor(heads * D, n, dtype, 100 * seed + 2 * i), _tensor(heads * D, n, dtype, 100 * seed + 2 * i + 1, 0)
             self.k.append(None), self.v.append(None)
             self.put(i, k, v)
-        fill = lambda rows: _int([r + [-7] * (max(max(len(x) for x in rows), 1) + spare - len(r)) for r in rows])
-        self.prefix_table, self.table = fill(rows[:len(prefixes)]), fill(rows[len(prefixes):])
+        spare = (1 << 27) // (len(own) * heads * 2 * D * page) if apart else 0
+        fill = lambda rows, spare=0: _int([r + [-7] * (max(len(x) for x in rows) + 1 + spare - len(r)) for r in rows])
+        self.prefix_table, self.table = fill(rows[:len(prefixes)], spare), fill(rows[len(prefixes):])
 
     def put(self, i, k, v):
         if k.shape[1]:
@@ -95,11 +97,12 @@ CASES = [  # prefixes, families, own, counts (None: one each), q heads, heads, D
 ]
 
 
+@pytest.mark.parametrize("apart", [False, True])
 @pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(x) for x in c[4:]) + "-%dx%d" % (max(c[0]), sum(c[1])))
-def test_definition(case):
+def test_definition(case, apart):
     prefixes, families, own, counts, q_heads, heads, D, page, fmt = case
-    announce("shared", *case)
-    s = Served(prefixes, families, own, heads, D, page, DTYPE[fmt])
+    announce("shared", *case, apart)
+    s = Served(prefixes, families, own, heads, D, page, DTYPE[fmt], apart=apart)
     n = counts or [1] * len(own)
     q = _tensor(q_heads * D, sum(n), DTYPE[fmt], 9)
     want, tol = s.want(q, n)
@@ -141,10 +144,11 @@ def test_like_a_table_that_names_the_prefix(fmt, D, q_heads, heads, batch, prefi
     assert (got - want).abs().mean() <= 2 * half * want.abs().mean() + 2.0 ** -14
 
 
-def test_pages_that_are_not_there_and_impossible_lengths():
+@pytest.mark.parametrize("apart", [False, True])
+def test_pages_that_are_not_there_and_impossible_lengths(apart):
     """They are NaN to those who see them, and to nobody else."""
-    announce("shared, bad pages")
-    s = Served([70, 40], [2, 2], [33, 20, 40, 10], 1, 64, 32, torch.float16)
+    announce("shared, bad pages", apart)
+    s = Served([70, 40], [2, 2], [33, 20, 40, 10], 1, 64, 32, torch.float16, apart=apart)
     q = _tensor(128, 4, torch.float16, 5)
     want, tol = s.want(q, [1] * 4)
     q = q.to(DEV)
@@ -153,22 +157,33 @@ def test_pages_that_are_not_there_and_impossible_lengths():
     bad = want.copy()
     bad[:, [0, 1, 3]] = NAN
     check(s.call(q), bad, tol, "missing pages")
-    s = Served([70, 40], [2, 2], [33, 20, 40, 10], 1, 64, 32, torch.float16)
+    s = Served([70, 40], [2, 2], [33, 20, 40, 10], 1, 64, 32, torch.float16, apart=apart)
     s.own[2], s.prefixes[0] = 32 * s.table.shape[1] + 1, 32 * s.prefix_table.shape[1] + 1
     bad = want.copy()
     bad[:, [0, 1, 2]] = NAN
-    check(s.call(q, max_length=64, max_prefix=96), bad, tol, "too long")
+    check(s.call(q, max_length=64), bad, tol, "too long")
+    # the same for many queries of a sequence
+    s = Served([70, 40], [1, 1], [60, 45], 1, 64, 32, torch.float16, apart=apart)
+    q, counts = _tensor(128, 65, torch.float16, 5), [25, 40]
+    want, tol = s.want(q, counts)
+    s.prefix_table[0, 2] = -1
+    want[:, :25] = NAN
+    check(s.call(q.to(DEV), counts), want, tol, "missing page, many queries")
+    s.table[1, 1] = 10 ** 6
+    want[:, 25 + 32 - 5:] = NAN                                     # own positions 32 and up
+    check(s.call(q.to(DEV), counts), want, tol, "missing own page, many queries")
 
 
-def test_nothing_to_see_and_infinities():
-    announce("shared, empty")
-    s = Served([0, 50], [2, 1], [0, 4, 0], 2, 64, 32, torch.bfloat16)
+@pytest.mark.parametrize("apart", [False, True])
+def test_nothing_to_see_and_infinities(apart):
+    announce("shared, empty", apart)
+    s = Served([0, 50], [2, 1], [0, 4, 0], 2, 64, 32, torch.bfloat16, apart=apart)
     q = _tensor(256, 3, torch.bfloat16, 6)
     want, tol = s.want(q, [1, 1, 1])
     assert (want[:, 0] == 0).all() and (want[:, 1:] != 0).any()
     check(s.call(q.to(DEV)), want, tol, "empty")
     # a block of values that is not finite, in the prefix of one family, is that family's
-    s = Served([40, 50], [1, 2], [3, 4, 5], 2, 64, 32, torch.bfloat16)
+    s = Served([40, 50], [1, 2], [3, 4, 5], 2, 64, 32, torch.bfloat16, apart=apart)
     k, v = _tensor(128, 50, torch.bfloat16, 7), _tensor(128, 50, torch.bfloat16, 8)
     v[70, 49] = INF
     s.put(1, k, v)
@@ -178,29 +193,32 @@ def test_nothing_to_see_and_infinities():
     check(got, want, tol, "infinity")
 
 
-@pytest.mark.parametrize("counts", [None, [2, 1, 3]])
-def test_columns_of_no_sequence_stay(counts):
+@pytest.mark.parametrize("apart", [False, True])
+@pytest.mark.parametrize("counts", [None, [2, 1, 3], [9, 0, 12], [20, 31, 33]])
+def test_columns_of_no_sequence_stay(counts, apart):
     """Columns before the first sequence's and behind the last one's, and what lies around the result."""
-    announce("shared, columns", counts)
+    announce("shared, columns", counts, apart)
     dtype = torch.float16
-    s = Served([600], [3], [20, 30, 40], 2, 64, 32, dtype)
+    s = Served([3000], [3], [20, 30, 40], 2, 64, 32, dtype, apart=apart)
     n = counts or [1, 1, 1]
     q = _tensor(256, sum(n), dtype, 5)
-    want = s.call(q.to(DEV), counts)
+    want, tol = s.want(q, n)
+    check(s.call(q.to(DEV), counts), want, tol, "as it is")
     wide = torch.full((256, sum(n) + 9), 3.0, dtype=dtype, device=DEV)
     wide[:, 4:4 + sum(n)] = q.to(DEV)
     starts = _int([4 + sum(n[:b]) for b in range(4)])
     memory = torch.full((256, sum(n) + 15), 5.0, dtype=dtype, device=DEV)
     out = memory[:, 3:-3]
     got = s.cache.shared_attention(wide, s.prefix_table, _int(s.prefixes), s.table, _int(s.own), starts=starts, max_queries=max(n), out=out)
-    assert got is out and torch.equal(out[:, 4:4 + sum(n)], want)
+    assert got is out
+    check(out[:, 4:4 + sum(n)], want, tol, "among others")          # (other bounds may cut the work otherwise)
     assert (memory[:, :7] == 5).all() and (memory[:, 7 + sum(n):] == 5).all()
 
 
 def test_bounds_of_the_host_that_are_too_small_or_too_large():
     """max_length and max_prefix decide how the work is cut only; larger max_queries and max_sharing change nothing."""
     announce("shared, bounds")
-    s = Served([3000], [3], [700, 30, 1], 1, 128, 32, torch.float16)
+    s = Served([3000], [3], [700, 30, 1], 1, 128, 32, torch.float16, apart=True)
     q = _tensor(512, 3, torch.float16, 5)
     want, tol = s.want(q, [1, 1, 1])
     for kw in (dict(max_length=1, max_prefix=1), dict(max_length=32 * s.table.shape[1], max_prefix=32 * s.prefix_table.shape[1], max_sharing=2 ** 31 - 1)):
@@ -208,14 +226,15 @@ def test_bounds_of_the_host_that_are_too_small_or_too_large():
     check(s.call(q.to(DEV), [1, 1, 1], max_sharing=1000), want, tol, "starts")
 
 
-def test_graphs_and_streams():
+@pytest.mark.parametrize("max_prefix", [500, None])
+def test_graphs_and_streams(max_prefix):
     """Two captured calls that share the allocator's pool, replayed in turn while lengths grow; and another stream."""
-    announce("shared, graphs")
+    announce("shared, graphs", max_prefix)
     dtype = torch.float16
-    s = Served([500], [4], [100, 20, 60, 90], 2, 64, 32, dtype)
+    s = Served([500], [4], [100, 20, 60, 90], 2, 64, 32, dtype, apart=True)
     prefix, own = _int([500]), _int([1, 1, 1, 1])
     qs = [_tensor(512, 4, dtype, 20 + i).to(DEV) for i in range(2)]
-    call = lambda q, **kw: s.cache.shared_attention(q, s.prefix_table, prefix, s.table, own, max_length=100, max_prefix=500, **kw)
+    call = lambda q, **kw: s.cache.shared_attention(q, s.prefix_table, prefix, s.table, own, max_length=100, max_prefix=max_prefix, **kw)
     for q in qs:
         call(q)
     torch.cuda.synchronize()
@@ -238,12 +257,20 @@ def test_graphs_and_streams():
     assert torch.equal(got, want)
 
 
-def test_kernels_of_both_parts():
-    """Few columns, many, and long prefixes in parts: the kernels that run."""
+def test_kernels_that_run():
+    """Few sequences behind short prefixes, many, and prompts: the kernels that run, and that they agree where the host's bounds choose between them."""
     announce("shared, kernels")
-    s = Served([200], [2], [5, 5], 1, 64, 32, torch.float16)
-    s.call(_tensor(64, 2, torch.float16, 1).to(DEV))
-    assert binding.last_kernel().startswith("shflbw_attention_decode_kernel<64,16 columns")
-    s = Served([200], [70], [5] * 70, 1, 64, 32, torch.float16)
-    s.call(_tensor(256, 70, torch.float16, 1).to(DEV))
-    assert binding.last_kernel().startswith("shflbw_attention_tile_kernel<64,cache")
+    name = lambda: binding.last_kernel()
+    s = Served([200], [70], [5] * 70, 1, 64, 32, torch.float16, apart=True)
+    q = _tensor(256, 70, torch.float16, 1)
+    want, tol = s.want(q, [1] * 70)
+    check(s.call(q.to(DEV), max_prefix=200, max_length=5), want, tol, "together")
+    assert name().startswith("shflbw_attention_decode_kernel<64,16 columns")
+    check(s.call(q.to(DEV), max_length=5), want, tol, "apart")
+    assert name().startswith("shflbw_attention_tile_kernel<64,cache")      # 280 columns of the prefix
+    s = Served([200], [20], [5] * 20, 1, 64, 32, torch.float16, apart=True)
+    s.call(_tensor(64, 20, torch.float16, 1).to(DEV))
+    assert name().startswith("shflbw_attention_decode_kernel<64,32 columns")
+    s = Served([200], [2], [30] * 2, 1, 64, 32, torch.float16)
+    s.call(_tensor(64, 40, torch.float16, 1).to(DEV), [20, 20])
+    assert name().startswith("shflbw_attention_tile_kernel<64,cache")
