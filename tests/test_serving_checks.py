@@ -128,12 +128,12 @@ def test_shared_attention_library_refuses():
     L, c = binding.lib(), binding._Cache(128, 8, 32, 2, 64, 0)
 
     def size(prefix=(), own=()):
-        p = dict(prefixes=1, table_pages=4, table_ld=4, max_length=128, max_tokens=3, table=None, lengths=None, members=None)
+        p = dict(prefixes=1, table_pages=1 << 20, table_ld=1 << 20, max_length=1 << 25, max_tokens=3, table=None, lengths=None, members=None)
         s = dict(q_heads=4, batch=3, max_queries=1, table_pages=4, window=0, sinks=0, tokens=3, max_length=128, table_ld=4, table=None, lengths=None, starts=None)
         p.update(prefix), s.update(own)
         return L.shflbw_kv_shared_attention_workspace(c, binding._Prefixes(**p), binding._Sequences(**s)), binding._Prefixes(**p), binding._Sequences(**s)
-    assert size()[0] >= 4 * 3 * 66 * 4 and size(own=dict(batch=0, tokens=0))[0] == 0
-    for bad in (dict(prefixes=0), dict(prefixes=2), dict(table_pages=0), dict(table_ld=3), dict(max_length=0), dict(max_length=129), dict(max_tokens=0),
+    assert size()[0] >= 4 * 3 * 66 * 4 and size(own=dict(batch=0, tokens=0))[0] == 0 and size(dict(max_length=100))[0] == 0
+    for bad in (dict(prefixes=0), dict(prefixes=2), dict(table_pages=0), dict(table_ld=3), dict(max_length=0), dict(max_length=(1 << 25) + 1), dict(max_tokens=0),
                 dict(table_pages=1 << 27, table_ld=1 << 27)):
         assert size(prefix=bad)[0] == BAD_SHAPE, bad
     for bad in (dict(window=1), dict(sinks=1), dict(q_heads=3), dict(max_length=0), dict(tokens=2), dict(max_queries=0)):
