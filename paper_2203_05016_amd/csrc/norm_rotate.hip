@@ -46,6 +46,16 @@ __device__ __forceinline__ uint16_t rot_narrow(float f)
     if constexpr (BF) return __builtin_bit_cast(uint16_t, (__bf16)f);
     else return __builtin_bit_cast(uint16_t, (_Float16)f);
 }
+// two values to 16 bits, to nearest even
+typedef float rot_float2 __attribute__((ext_vector_type(2)));
+typedef _Float16 rot_half2 __attribute__((ext_vector_type(2)));
+typedef __bf16 rot_bf2 __attribute__((ext_vector_type(2)));
+template <bool BF>
+__device__ __forceinline__ unsigned rot_pack(float a, float b)
+{
+    if constexpr (BF) return __builtin_bit_cast(unsigned, __builtin_convertvector((rot_float2{a, b}), rot_bf2));
+    else return __builtin_bit_cast(unsigned, __builtin_convertvector((rot_float2{a, b}), rot_half2));
+}
 // the features of pair n: those past 2 * pairs are pairs of neighbours that are not turned
 struct RotPair {
     int a, b;
@@ -73,6 +83,13 @@ __device__ __forceinline__ float2 rot_turn(float half)
     const int q = (int)quarter;
     const float cosine = q & 1 ? s : c, sine = q & 1 ? c : s;
     return float2{(q + 1) & 2 ? -cosine : cosine, q & 2 ? -sine : sine};
+}
+// turns (u, v) by the angle of cosine c.x and sine c.y; the same roundings wherever it is called
+__device__ __forceinline__ void rot_pair(float& u, float& v, float2 c)
+{
+    const float turned = __builtin_fmaf(u, c.x, -(v * c.y));
+    v = __builtin_fmaf(u, c.y, v * c.x);
+    u = turned;
 }
 // cosine and sine of pair n at a token's position
 __device__ __forceinline__ float2 rot_angle(const RotateArgs& a, int n, int64_t token)
@@ -203,10 +220,7 @@ __global__ __launch_bounds__(256) void norm_rotate_few_kernel(RotateArgs a)
             const float2 w = weight[kind][n];
             float u = rot_widen<BF>(x[i] & 0xffffu) * by.first * by.second * w.x, v = rot_widen<BF>(x[i] >> 16) * by.first * by.second * w.y;
             if (n < a.pairs) {
-                const float2 c = angle[n][t];
-                const float turned = u * c.x - v * c.y;
-                v = u * c.y + v * c.x;
-                u = turned;
+                rot_pair(u, v, angle[n][t]);
             }
             if (token0 + t < a.tokens) {
                 dst[f.a * a.ld_out[kind]] = rot_narrow<BF>(u);
@@ -298,6 +312,9 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(RotateArgs a)
             by[e] = rot_root<D>(sum, (float)a.eps);
         }
         if (__all(ordinary)) {
+            // (what was widened for the sums is widened again, not kept: bfloat16 heads of 128 took 254 registers)
+#pragma unroll
+            for (int i = 0; i < P; ++i) asm volatile("" : "+v"(x[i][0]), "+v"(x[i][1]));
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 const int n = i * PARTS + part;
@@ -314,11 +331,8 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(RotateArgs a)
 #pragma unroll
                     for (int e = 0; e < 8; e += 2) {
                         const float4 t = c[e / 2];
-                        const float y = u[e] * t.x - v[e] * t.y, z = u[e + 1] * t.z - v[e + 1] * t.w;
-                        v[e] = u[e] * t.y + v[e] * t.x;
-                        v[e + 1] = u[e + 1] * t.w + v[e + 1] * t.z;
-                        u[e] = y;
-                        u[e + 1] = z;
+                        rot_pair(u[e], v[e], float2{t.x, t.y});
+                        rot_pair(u[e + 1], v[e + 1], float2{t.z, t.w});
                     }
                 }
                 uint16_t* p = dst + (f.a * ld_out + from);
@@ -326,8 +340,8 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(RotateArgs a)
                 rot4 y, z;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    y[e] = rot_narrow<BF>(u[2 * e]) | (unsigned)rot_narrow<BF>(u[2 * e + 1]) << 16;
-                    z[e] = rot_narrow<BF>(v[2 * e]) | (unsigned)rot_narrow<BF>(v[2 * e + 1]) << 16;
+                    y[e] = rot_pack<BF>(u[2 * e], u[2 * e + 1]);
+                    z[e] = rot_pack<BF>(v[2 * e], v[2 * e + 1]);
                 }
                 if (skip == 0) {
                     rot_store<STREAM>(p, y);
@@ -368,12 +382,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(RotateArgs a)
                 const float2 w = weight[kind][n];
                 float u = rot_widen<BF>(src[f.a * ld_in + from + e]) * factor.first * factor.second * w.x;
                 float v = rot_widen<BF>(src[f.b * ld_in + from + e]) * factor.first * factor.second * w.y;
-                if (n < a.pairs) {
-                    const float2 t = angle[n][8 * run + e];
-                    const float y = u * t.x - v * t.y;
-                    v = u * t.y + v * t.x;
-                    u = y;
-                }
+                if (n < a.pairs) rot_pair(u, v, angle[n][8 * run + e]);
                 if (e >= skip) {
                     dst[f.a * ld_out + from + e] = rot_narrow<BF>(u);
                     dst[f.b * ld_out + from + e] = rot_narrow<BF>(v);
@@ -396,8 +405,8 @@ int launch(RotateArgs a, hipStream_t stream)
     // are most of what few tokens take.
     const int64_t work = a.tokens * a.all_heads;
     const bool many = near && a.tokens >= 8 && work > 18000;
-    // Results of 16 MB and more leave past the L2s, if in whole 64 bytes: 72 by 8192 59 us, through them 76, by 1024 10.5 and 12.8, by 8191, in parts of lines, 136
-    // and 89.  Such rows take 64 tokens to a wavefront where there are many, 83 (by 2048 28, of 32 21).
+    // Results of 16 MB and more leave past the L2s, if in whole 64 bytes: 72 by 8192 60 us, through them 76, by 1024 10.4 and 12.8, by 8191, in parts of lines, 136
+    // and 91.  Such rows take 64 tokens to a wavefront where there are many, 80 (by 2048 28, of 32 21).
     const bool stream_out = whole && work * D * 2 >= 16 << 20, wide = !whole && work >= 300000;
     const int T = many ? (wide ? 64 : 32) : work <= 6000 ? 4 : 8;
     const int64_t eighth = (a.tokens + 8 * T - 1) / (8 * T);

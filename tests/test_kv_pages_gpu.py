@@ -259,6 +259,25 @@ def test_compact(pages, page, width, rows, heads, D, share):
             assert (t._base.view(rows, ld)[:, width:] == 77).all()
 
 
+def test_pages_past_four_gigabytes():
+    announce("pages, far")
+    c = binding.KVCache(40000, 64, 16, 128, torch.float16, DEV)     # 5.6 GB
+    g = torch.Generator().manual_seed(5)
+    some = torch.randint(0, 256, (3, c.data.shape[1]), generator=g, dtype=torch.uint8).to(DEV)
+    for i, p in enumerate((39999, 39998, 35001)):
+        c.data[p].copy_(some[i])
+    uses = torch.zeros(40000, dtype=torch.int32, device=DEV)
+    uses[[39999, 39998, 35001]] = 1
+    uses[:35000] = 3                                                # other tables' pages
+    table, lengths = dev([[39999, 39998], [35001, -1]]), dev([100, 64])
+    got = c.fork(table, lengths, uses, dev([0, 0, 1]))
+    assert got[0].tolist() == [[39999, 39998], [39999, 35000], [35001, -1]] and torch.equal(c.data[35000], some[1])
+    small, now = c.compact(got[0], got[2])
+    assert small.tolist() == [[35003, 35002], [35003, 35000], [35001, -1]]
+    assert torch.equal(c.data[35003], some[0]) and torch.equal(c.data[35002], some[1]) and torch.equal(c.data[35001], some[2])
+    assert now[35000:35005].tolist() == [1, 1, 1, 2, 0] and int((now > 0).sum()) == 35004
+
+
 def test_page_that_no_count_knows_stays():
     announce("compact stale")
     c = cache_of(8)

@@ -194,6 +194,26 @@ def test_rotation_keeps_products_of_equal_distance():
     assert (a[0] - a[0, 0]).abs().max() > 1
 
 
+def test_rows_that_are_far_apart():
+    """Offsets past 32 bits: rows of 2^23 tokens and more, of which a few thousand are taken, where runs of 16 bytes are not, and 2^25 of a head's bytes apart."""
+    announce("norm_rotate far rows")
+    D, dtype, f = 64, torch.float16, frequencies(32)
+    for ld, tokens in (((1 << 23) + 40, 19000), ((1 << 23) - 8, 9001)):
+        memory = torch.zeros(3 * D * ld, dtype=dtype, device=DEV)
+        rows = memory.view(3 * D, ld)[:, ld - tokens:]              # the last columns
+        x = tensor(3 * D, tokens, dtype, 3)
+        rows.copy_(x)
+        p = positions(tokens)
+        q, k = rows[:2 * D], rows[2 * D:]
+        want = binding.norm_rotate(x[:2 * D], x[2 * D:], D, p, f)
+        binding.norm_rotate(q, k, D, p, f, q_out=q, k_out=k)
+        for got, y in ((q, want[0]), (k, want[1])):
+            assert (got.double() - y.double()).abs().max() <= 2 ** -9    # the other kernel's sums: a step of results below 4 at most
+        check(q[:D, -50:], definition(x[:D, -50:], D, p[-50:], f), "far rows")
+        assert (memory.view(3 * D, ld)[:, :ld - tokens] == 0).all()
+        del memory, rows, q, k
+
+
 def test_nothing_to_do():
     announce("norm_rotate nothing")
     f = frequencies(32)
