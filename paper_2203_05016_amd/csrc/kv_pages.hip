@@ -3,7 +3,9 @@
 // arguments alone: free (or used) pages are counted by blocks of PAGES_BLOCK of them, every block adds up the counts of those before it, and
 // ranks inside a block come from ballots.  Atomic additions are of whole numbers, whose order does not show.
 //
-// Bound by latency (a launch for every step that needs all of the step before) but for the pages that are copied.
+// Bound by latency (a launch for every step that needs all of the step before, 3 to 5 us each on the GPU, of which most is the chain of loads and barriers) but
+// for the pages that are copied.  64 sequences, one token more, 8192 pages: 9.6 us; 256 prompts of up to 8192 tokens, 65536 pages: 15.4; 512 sequences continued by
+// 8 each, 16000 pages, 15 MB copied: 17; 2000 of 8000 pages of 70 KB to the front: 51 us, 5.4 TB/s (a large copy 5.2).
 #include <hip/hip_runtime.h>
 
 #include <climits>
@@ -19,9 +21,11 @@ namespace {
 constexpr int PAGES_BLOCK = 4096;          // pages to a workgroup of 1024 threads
 constexpr int COPY_BYTES = 16384;          // bytes of a page to a workgroup of 256 threads
 constexpr int MOST_BLOCKS = 16384;         // of a launch whose workgroups take pieces in turn
-constexpr int FEW_PAGES = 16384;           // of a cache whose books one workgroup keeps
+// What one workgroup does alone, in fewer launches: pages that it ranks, rows that it has in the LDS, entries and slots that it works out.  16 rows of
+// 64 pages forked 9.4 us, one token more 7.3, where five and three launches take 20 and 12; 128 rows 16.9 and 13.2, in several launches 12.4 and 10.6.
+constexpr int FEW_PAGES = 16384;
 constexpr int FEW_ROWS = 2048;
-constexpr int64_t FEW_ENTRIES = 32768;     // entries, and slots, that it works out
+constexpr int64_t FEW_ENTRIES = 8192;
 static_assert(PAGES_BLOCK == 4 * 1024, "rank_flags takes four runs of 1024");
 
 typedef unsigned copy4 __attribute__((ext_vector_type(4)));
@@ -161,13 +165,13 @@ __device__ __forceinline__ int rank_block(const PagesArgs& a, const int32_t* use
 struct FewUses {
     int of[FEW_PAGES / 1024];
 };
-__device__ __forceinline__ FewUses load_few(const PagesArgs& a)
+__device__ __forceinline__ FewUses load_few(const PagesArgs& a, const int32_t* uses)
 {
     FewUses u;
 #pragma unroll
     for (int i = 0; i < FEW_PAGES / 1024; ++i) {
         const int p = i * 1024 + (int)threadIdx.x;
-        u.of[i] = a.uses_in[p < a.pages ? p : a.pages - 1];
+        u.of[i] = uses[p < a.pages ? p : a.pages - 1];
     }
     return u;
 }
@@ -217,6 +221,15 @@ __global__ __launch_bounds__(1024) void pages_take_kernel(PagesArgs a, const int
         if (p < a.pages) take_page(a, a.list, wanted, p, free, rank, uses[p]);
     });
     if (blockIdx.x == 0 && threadIdx.x == 0) a.totals[FREE] = n.all;
+}
+// by one workgroup, without the counts of another launch
+__global__ __launch_bounds__(1024) void pages_take_few_kernel(PagesArgs a, const int32_t* uses)
+{
+    __shared__ int64_t shared[64];
+    const FewUses u = load_few(a, uses);
+    const int wanted = a.totals[WANTED];
+    const int free = rank_few<false>(a, u, shared, [&](int p, bool is_free, int rank, int n) { take_page(a, a.list, wanted, p, is_free, rank, n); });
+    if (threadIdx.x == 0) a.totals[FREE] = free;
 }
 // the page of rank `rank` among those taken, or -1
 __device__ __forceinline__ int taken_page(const PagesArgs& a, int64_t rank, int free) { return rank < free ? a.list[rank] : -1; }
@@ -287,7 +300,7 @@ __global__ __launch_bounds__(1024) void extend_few_kernel(PagesArgs a)
 {
     __shared__ int64_t shared[64];
     __shared__ int32_t list[FEW_PAGES], base[FEW_ROWS], old_length[FEW_ROWS], length[FEW_ROWS], starts[FEW_ROWS + 1];
-    const FewUses uses = load_few(a);
+    const FewUses uses = load_few(a, a.uses_in);
     PagesArgs b = a;
     b.list = list;
     b.base = base;
@@ -502,7 +515,7 @@ __global__ __launch_bounds__(1024) void compact_rank_kernel(PagesArgs a)
 __global__ __launch_bounds__(1024) void compact_few_kernel(PagesArgs a)
 {
     __shared__ int64_t shared[64];
-    const FewUses uses = load_few(a);
+    const FewUses uses = load_few(a, a.uses_in);
     int n = 0;
 #pragma unroll
     for (int i = 0; i < FEW_PAGES / 1024; ++i) n += i * 1024 + (int)threadIdx.x < a.pages && uses.of[i] != 0;
@@ -675,8 +688,12 @@ int shflbw_kv_fork(const shflbw_kv_cache* cache, const shflbw_kv_pages* in, cons
     }
     hipLaunchKernelGGL(fork_count_kernel, dim3(a.uses_in == a.uses_out ? 1 : 1 + few_blocks(ceil_div(a.pages, 1024))), dim3(1024), 0, st, a);
     hipLaunchKernelGGL(fork_table_kernel, dim3(few_blocks(ceil_div(((int64_t)a.rows_in + a.rows) * a.width, 256))), dim3(256), 0, st, a);
-    hipLaunchKernelGGL(pages_count_kernel, dim3(a.page_blocks), dim3(1024), 0, st, a);
-    hipLaunchKernelGGL(pages_take_kernel, dim3(a.page_blocks), dim3(1024), 0, st, a, a.uses_out);
+    if (a.pages <= FEW_PAGES) {
+        hipLaunchKernelGGL(pages_take_few_kernel, dim3(1), dim3(1024), 0, st, a, a.uses_out);
+    } else {
+        hipLaunchKernelGGL(pages_count_kernel, dim3(a.page_blocks), dim3(1024), 0, st, a);
+        hipLaunchKernelGGL(pages_take_kernel, dim3(a.page_blocks), dim3(1024), 0, st, a, a.uses_out);
+    }
     hipLaunchKernelGGL(fork_copy_kernel, dim3(few_blocks((int64_t)a.rows * parts)), dim3(256), 0, st, a, parts);
     return launched();
 }
