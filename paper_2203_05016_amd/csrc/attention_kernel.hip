@@ -558,6 +558,38 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
             }
             __syncthreads();
         }
+        if (joined) {
+            // A wavefront to a column: lanes take four neighbouring features of every UNITS-th part, so that all of a column's parts travel at once
+            constexpr int LANES = D / 4, UNITS = 64 / LANES;
+            const int unit = lane / LANES, f = 4 * (lane % LANES);
+            const int64_t step = (int64_t)a.heads * a.group * a.tokens * D;
+            for (int c = wave; c < 16 && 16 * n + c < cols; c += W) {
+                const int64_t at = where[16 * n + c];
+                const float* w = weight + c * (ATTN_JOINED + 1);
+                float4v x = {0, 0, 0, 0};
+                if (unit < UNITS) {
+                    const float* from = a.joined_o + attn_row(a, at) * D + f;
+#pragma unroll 8
+                    for (int i = unit; i < a.joined; i += UNITS) x += *reinterpret_cast<const float4v*>(from + i * step) * w[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (LANES == 24) x[i] += __shfl(x[i], lane + 24 < 64 ? lane + 24 : lane);
+                    else
+#pragma unroll
+                        for (int by = LANES; by < 64; by *= 2) x[i] += __shfl_xor(x[i], by);
+                }
+                if (unit == 0) {
+                    float4v own_sum = {0, 0, 0, 0};
+#pragma unroll
+                    for (int i = 0; i < W; ++i) own_sum += *reinterpret_cast<const float4v*>(sums + (i * 16 + c) * OP + f);
+                    x += own_sum * w[ATTN_JOINED];
+                    uint16_t* dst = a.out + ((at >> 32) * D + f) * a.ldo + (at & 0xffffffffLL);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dst[i * a.ldo] = attn_narrow<BF>(x[i]);
+                }
+            }
+        } else
 #pragma unroll
         for (int k = 0; k < 16 * D / (64 * W); ++k) {
             const int e = threadIdx.x + k * 64 * W, c = e / D, d = e % D, at = 16 * n + c;
@@ -565,16 +597,7 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
             float x = 0;
 #pragma unroll
             for (int i = 0; i < W; ++i) x += sums[(i * 16 + c) * OP + d];
-            if (joined) {
-                const float* w = weight + c * (ATTN_JOINED + 1);
-                const float* from = a.joined_o + attn_row(a, where[at]) * D + d;
-                const int64_t step = (int64_t)a.heads * a.group * a.tokens * D;
-                x *= w[ATTN_JOINED];
-#pragma unroll 8
-                for (int i = 0; i < a.joined; ++i, from += step) x += *from * w[i];
-            }
-            if (joined) a.out[((where[at] >> 32) * D + d) * a.ldo + (where[at] & 0xffffffffLL)] = attn_narrow<BF>(x);
-            else if (!a.part_o) a.out[where[at] + d * a.ldo] = attn_narrow<BF>(x);
+            if (!a.part_o) a.out[where[at] + d * a.ldo] = attn_narrow<BF>(x);
             else a.part_o[where[at] * D + d] = x;
         }
         __syncthreads();

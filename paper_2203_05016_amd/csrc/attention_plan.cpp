@@ -137,11 +137,9 @@ SharedPlan plan_shared_attention(int prefixes, int64_t max_sharing, int64_t max_
     }
     p.prefix = plan_prefix((int64_t)prefixes * heads, group, D, max_sharing, max_prefix);
     p.own = plan_cache_attention(batch, heads, group, D, tokens, max_queries, max_length, INT32_MAX, 0);
-    // The kernel for few queries joins the prefixes' parts with what it finds, if there are no parts of its own keys, and if what a workgroup then
-    // fetches is little: 64 sequences, 64 heads over 8 of 128, 16 parts 46 us, by a kernel of its own 54; 8 with 32 parts 26 and 25; 8 queries of each of
-    // 64, 8 parts, 125 and 115.
-    const int64_t fetched = (int64_t)std::min(16 * p.own.col_tiles, group * max_queries) * p.prefix.splits * D * 4;
-    p.joins = p.own.decode && p.own.splits == 1 && p.prefix.splits <= ATTN_JOINED && fetched <= (p.own.groups >= CUS ? 65536 : 16384);
+    // The kernel for few queries joins the prefixes' parts with what it finds, if there are no parts of its own keys: 64 sequences, 64 heads over 8 of 128, 16 parts
+    // 46 us, by a kernel of its own 55; 8 with 32 parts 28.2 and 30.1; 128 of 32 over 8 of 96 27 and 33; 8 queries of each of 64 113 and 115.
+    p.joins = p.own.decode && p.own.splits == 1 && p.prefix.splits <= ATTN_JOINED;
     p.workspace = parts((int64_t)p.prefix.splits + (p.joins ? 0 : p.own.splits));
     return p;
 }
