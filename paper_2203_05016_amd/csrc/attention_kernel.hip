@@ -248,6 +248,10 @@ __device__ __forceinline__ float attn_max3(float a, float b, float c) { return f
 // 2 of 131071 keys (f16, 277 MB) 48 us, 5.8 TB/s (part of it lies in the memory-side cache), and 4.2 for the join; 128 under a window of
 // 1024 with 4 sinks, 16 heads of 64, 144 MB: 30 us, 4.7 TB/s.  Vector instructions are issued in 32 % of the cycles, the matrix units busy in 10.
 // With 5 queries each (48 columns; 24 sequences of up to 3001 keys, 56 MB) 34 us: a CU has 8 wavefronts, half of the CUs none.
+//
+// Calls with prefixes: a sequence's keys behind its prefix's (4 sequences behind 601 keys, 16 heads of 64, 7.3 us); or all columns of a prefix, which see all of its keys, as parts (16
+// prefixes of 4096, 96 columns of heads of 96 in blocks of 48, 36 us: latency of unpacking, exponentials and products in turn, two wavefronts a SIMD); or
+// own keys, joined with the prefixes' parts (64 sequences of up to 512 keys, 16 parts: 16 us, 34 of the 54 MB read are the parts).
 template <bool BF, int D, int NT, int W, class CALL>
 __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_decode_kernel(AttnArgs a)
 {
@@ -623,6 +627,9 @@ __global__ __launch_bounds__(64 * W, decode_residency(NT, D)) void attention_dec
 // units are busy in 52, 44 and 30 % of the cycles, vector instructions issued in 53, 48 and 65 %; the clock is at 2.1 GHz (1.8 in the first dozen
 // launches after a pause, which take up to 18 % longer).  Prompts are further from their floor than chunks: half as many tiles a workgroup, so that first loads and
 // last stores weigh more, and heads of 128 in workgroups of 8 spill 74 registers (300 bytes a lane), which chunks do not.
+//
+// Calls with prefixes: sequences behind their prefix, whose keys are the first (8 of 512 queries behind 4096 tokens, 64 heads over 8 of 128, 522 us, 1.1 PFLOP/s); or
+// all columns of a prefix, of all of a key head's query heads in a row, as parts (64 sequences behind 8001: 29 us, 14 of them products; 34 MB of parts).
 //
 // Infinities and NaN among the values of a tile that not all of the workgroup's queries see whole are zeros in the LDS, so that
 // they do not reach a query that does not see them as 0 * NaN; if there were any, they are added where they are seen at the end.  In tiles that all
