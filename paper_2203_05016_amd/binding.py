@@ -639,7 +639,7 @@ class KVCache:
 
     def shared_attention(self, q, prefix_table, prefix_lengths, table, lengths, members=None, starts=None, max_queries=1, max_length=None,
                          max_prefix=None, max_sharing=None, out=None, stream=None):
-        """Attention of sequences that share prefixes, each of which is read once for all of them.
+        """Attention of sequences that share prefixes: a long one is read from memory once for all of them.
 
         q, table, lengths, starts, max_queries and max_length are those of ``attention``, the table and lengths those of the sequences' own tokens: every query
         sees its prefix whole, and its sequence's own tokens up to its own.  prefix_table (prefixes, pages) and prefix_lengths (prefixes,)

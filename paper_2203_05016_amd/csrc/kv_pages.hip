@@ -39,7 +39,7 @@ struct PagesArgs {
     int32_t *slots, *starts;
     char* data;
     int64_t ld_in, ld_out, tokens, page_bytes;
-    int rows_in, rows, width, pages, page_shift, blocks, page_blocks;
+    int rows_in, rows, width, pages, page_shift, page_blocks;
     // workspace: see carve
     int32_t *counts, *list, *source, *rank, *moved, *totals, *base, *old_length, *first, *children;
 };
