@@ -4,7 +4,7 @@
 // ranks inside a block come from ballots.  Atomic additions are of whole numbers, whose order does not show.
 //
 // Bound by latency (a launch for every step that needs all of the step before, 3 to 5 us each on the GPU, of which most is the chain of loads and barriers) but
-// for the pages that are copied.  64 sequences, one token more, 8192 pages: 9.6 us; 256 prompts of up to 8192 tokens, 65536 pages: 15.4; 512 sequences continued by
+// for the pages that are copied.  64 sequences, one token more, 8192 pages: 7.7 us; 256 prompts of up to 8192 tokens, 65536 pages: 15.4; 512 sequences continued by
 // 8 each, 16000 pages, 15 MB copied: 17; 2000 of 8000 pages of 70 KB to the front: 51 us, 5.4 TB/s (a large copy 5.2).
 #include <hip/hip_runtime.h>
 
@@ -22,7 +22,7 @@ constexpr int PAGES_BLOCK = 4096;          // pages to a workgroup of 1024 threa
 constexpr int COPY_BYTES = 16384;          // bytes of a page to a workgroup of 256 threads
 constexpr int MOST_BLOCKS = 16384;         // of a launch whose workgroups take pieces in turn
 // What one workgroup does alone, in fewer launches: pages that it ranks, rows that it has in the LDS, entries and slots that it works out.  16 rows of
-// 64 pages forked 9.4 us, one token more 7.3, where five and three launches take 20 and 12; 128 rows 16.9 and 13.2, in several launches 12.4 and 10.6.
+// 64 pages forked 9.4 us, one token more 6.5, where five and three launches take 20 and 12; 128 rows 16.9 and 10.2, in several launches 12.2 and 9.3.
 constexpr int FEW_PAGES = 16384;
 constexpr int FEW_ROWS = 2048;
 constexpr int64_t FEW_ENTRIES = 8192;
@@ -76,14 +76,20 @@ __device__ __forceinline__ int wave_sum(int x)               // over this lane a
     x += moved_lanes<0x143, 0xc>(x);                         // the last of 1 to 2 and 3
     return x;
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t moved_lanes64(int64_t x)
+{
+    const unsigned low = (unsigned)moved_lanes<CTRL, ROWS>((int)x);
+    return (int64_t)moved_lanes<CTRL, ROWS>((int)(x >> 32)) << 32 | low;
+}
 __device__ __forceinline__ int64_t wave_sum64(int64_t x)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int by = 1; by < 64; by *= 2) {
-        const int64_t y = __shfl_up(x, by);
-        if (lane >= by) x += y;
-    }
+    x += moved_lanes64<0x111, 0xf>(x);
+    x += moved_lanes64<0x112, 0xf>(x);
+    x += moved_lanes64<0x114, 0xf>(x);
+    x += moved_lanes64<0x118, 0xf>(x);
+    x += moved_lanes64<0x142, 0xa>(x);
+    x += moved_lanes64<0x143, 0xc>(x);
     return x;
 }
 // the sum of x over the threads before this one, and over all
@@ -261,6 +267,31 @@ __device__ __forceinline__ int64_t extend_rows(const PagesArgs& a, int64_t* shar
     if (threadIdx.x == 0) a.starts[a.rows] = tokens < INT_MAX ? (int)tokens : INT_MAX;
     return pages;
 }
+// What a row had and where its new pages are: entry j is the old one below `old`, a fresh one below `now`
+struct ExtendedRow {
+    int length, old, now;
+    int64_t base;
+};
+__device__ __forceinline__ ExtendedRow extended_row(const PagesArgs& a, int b)
+{
+    ExtendedRow r;
+    r.length = a.old_length[b];
+    r.old = held(a, r.length);
+    r.now = held(a, a.lengths_out[b]);
+    r.base = (int64_t)a.base[b] - r.old;
+    return r;
+}
+__device__ __forceinline__ int extended_entry(const PagesArgs& a, const ExtendedRow& r, int b, int j, int free)
+{
+    return j < r.old ? a.table_in[b * a.ld_in + j] : j < r.now ? taken_page(a, r.base + j, free) : -1;
+}
+// the slot of new token t of row b
+__device__ __forceinline__ int extended_slot(const PagesArgs& a, const ExtendedRow& r, int b, int64_t t, int free)
+{
+    const int64_t at = r.length + (t - a.starts[b]), j = at >> a.page_shift;
+    const int page = j < a.width ? extended_entry(a, r, b, (int)j, free) : -1;
+    return in_cache(a, page) ? (page << a.page_shift) + (int)(at & ((1 << a.page_shift) - 1)) : -1;
+}
 // A row's entries and its tokens' slots, by `step` threads of which this is `first`.  Row a.rows is that of the slots past the last token.
 __device__ __forceinline__ void extend_row(const PagesArgs& a, int b, int free, int first, int step)
 {
@@ -268,18 +299,10 @@ __device__ __forceinline__ void extend_row(const PagesArgs& a, int b, int free, 
         for (int64_t t = (int64_t)a.starts[b] + first; t < a.tokens; t += step) a.slots[t] = -1;
         return;
     }
-    const int length = a.old_length[b], old = held(a, length), now = held(a, a.lengths_out[b]);
-    const int64_t base = (int64_t)a.base[b] - old;
-    const int32_t* in = a.table_in + b * a.ld_in;
-    int32_t* out = a.table_out + b * a.ld_out;
-    const auto entry = [&](int j) __attribute__((always_inline)) { return j < old ? in[j] : taken_page(a, base + j, free); };
-    for (int j = first; j < a.width; j += step) out[j] = j < now ? entry(j) : -1;
+    const ExtendedRow r = extended_row(a, b);
+    for (int j = first; j < a.width; j += step) a.table_out[b * a.ld_out + j] = extended_entry(a, r, b, j, free);
     const int64_t start = a.starts[b], end = a.starts[b + 1] < a.tokens ? a.starts[b + 1] : a.tokens;
-    for (int64_t t = start + first; t < end; t += step) {
-        const int64_t at = length + (t - start), j = at >> a.page_shift;
-        const int page = j < a.width ? entry((int)j) : -1;
-        a.slots[t] = in_cache(a, page) ? (page << a.page_shift) + (int)(at & ((1 << a.page_shift) - 1)) : -1;
-    }
+    for (int64_t t = start + first; t < end; t += step) a.slots[t] = extended_slot(a, r, b, t, free);
 }
 __global__ __launch_bounds__(1024) void extend_count_kernel(PagesArgs a)
 {
@@ -315,7 +338,38 @@ __global__ __launch_bounds__(1024) void extend_few_kernel(PagesArgs a)
         if (i < a.rows) a.lengths_out[i] = length[i];
         a.starts[i] = starts[i];
     }
-    for (int row = threadIdx.x >> 6; row <= a.rows; row += 16) extend_row(b, row, free, threadIdx.x & 63, 64);
+    // four entries at a time, whose loads travel together, whatever rows they are of
+    const int entries = a.rows * a.width, all = entries + (int)a.tokens;     // (FEW_ENTRIES at most)
+    for (int e0 = threadIdx.x; e0 < all; e0 += 4096) {
+        int x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int e = e0 + k * 1024;
+            x[k] = -1;
+            if (e < entries) {
+                const int row = (unsigned)e / (unsigned)a.width;
+                x[k] = extended_entry(b, extended_row(b, row), row, e - row * a.width, free);
+            } else if (e < all && e - entries < starts[a.rows]) {
+                int low = 0, high = a.rows;                // starts[low] <= t < starts[high]
+                while (high - low > 1) {
+                    const int mid = (low + high) / 2;
+                    if (starts[mid] <= e - entries) low = mid;
+                    else high = mid;
+                }
+                x[k] = extended_slot(b, extended_row(b, low), low, e - entries, free);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int e = e0 + k * 1024;
+            if (e < entries) {
+                const int row = (unsigned)e / (unsigned)a.width;
+                a.table_out[row * a.ld_out + e - row * a.width] = x[k];
+            } else if (e < all) {
+                a.slots[e - entries] = x[k];
+            }
+        }
+    }
 }
 
 // ---- sequences that continue others
