@@ -10,8 +10,8 @@
 // Everything between the loads and the one rounding at the store is in 32 bits.  Squares of bfloat16 may be more than 32 bits hold, or, with an
 // eps that is as small, less: such columns' sums are done again in 64, and the factor is applied in two steps.
 //
-// Bound by memory: 4 bytes for each value.  72 heads of 128 (bf16) by 8192 tokens, 302 MB, 60 us, 5.0 TB/s, where a large copy moves 5.2; by 8191, whose rows are in no
-// alignment, 80 (lines are written in parts: 175 MB each way); by 64, 5.6, a launch and one chain of latencies.
+// Bound by memory: 4 bytes for each value.  72 heads of 128 (bf16) by 8192 tokens, 302 MB, 56 us, 5.4 TB/s (of inputs that no cache holds 72,
+// 4.2 TB/s), where a large copy moves 5.2; by 8191, whose rows are in no alignment, 76 and 87 (lines are written in parts: 175 MB each way); by 64, 5.6, a launch and one chain of latencies.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -408,13 +408,14 @@ int launch(RotateArgs a, hipStream_t stream)
     // are most of what few tokens take.
     const int64_t work = a.tokens * a.all_heads;
     const bool many = near && a.tokens >= 8 && work > 18000;
-    // Results of 16 MB and more leave past the L2s, if in whole 64 bytes: 72 by 8192 60 us, through them 76, by 1024 10.4 and 12.8, by 8191, in parts of lines, 136
-    // and 91.  Such rows take 64 tokens to a wavefront where there are many, 80 (by 2048 28, of 32 21).
+    // Results of 16 MB and more leave past the L2s, if in whole 64 bytes: 72 by 8192 56 us, through them 76, by 1024 10.4 and 12.8, by 8191, in parts of lines, 136
+    // and 91.  Such rows take 64 tokens to a wavefront where there are many, 76, of 32 82 (by 2048 28 and 21).
     const bool stream_out = whole && work * D * 2 >= 16 << 20, wide = !whole && work >= 300000;
     const int T = many ? (wide ? 64 : 32) : work <= 6000 ? 4 : 8;
     const int64_t eighth = (a.tokens + 8 * T - 1) / (8 * T);
-    // heads to a workgroup: as many as leave 1024 workgroups, the same number to each
-    const int64_t steps = ((int64_t)a.all_heads + 3) / 4, wanted = (1024 + 8 * eighth - 1) / (8 * eighth), each = (steps + wanted - 1) / wanted;
+    // heads to a workgroup: as many as leave 4096 workgroups, the same number to each.  72 heads of 128 by 8191, 8192 and 4099 tokens that no cache holds:
+    // 87, 72 and 50 us, with 1024 workgroups 95, 84 and 55, with 512 99, 84 and 58; with four heads to each 88, 74 and 50.
+    const int64_t steps = ((int64_t)a.all_heads + 3) / 4, wanted = (4096 + 8 * eighth - 1) / (8 * eighth), each = (steps + wanted - 1) / wanted;
     const int64_t parts = (steps + each - 1) / each, blocks = 8 * eighth * parts;
     if (blocks > 0x7fffffffLL) return fail(SHFLBW_ERR_BAD_SHAPE, "grid too large");
     a.eighth = (unsigned)eighth;
