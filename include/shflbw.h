@@ -440,7 +440,7 @@ int64_t shflbw_kv_pages_workspace(const shflbw_kv_cache* cache, int sequences);
 /*
  * More tokens for every sequence: sequence b gets counts[b] (device; below 0 is none), the pages it lacks for them, in order of
  * sequence and position, and their slots.
- *  in, out  of one shape; every array of out is the same as in's (in place) or overlaps none of them
+ *  in, out  of one shape; every array of out is the same as in's (in place) or overlaps none of them; none overlaps counts
  *  slots    device, tokens: the slots of the new tokens, sequence after sequence, to be written to; -1 where there is no page, and
  *           past the last token.  Tokens past `tokens` have no slot.
  *  starts   device, sequences + 1: where each sequence's begin (shflbw_kv_sequences.starts of their queries)
@@ -454,7 +454,7 @@ int shflbw_kv_extend(const shflbw_kv_cache* cache, const shflbw_kv_pages* in, co
  * in's rows leaves row i without tokens).  Full pages are shared.  A last page that is not full is kept by the
  * lowest i that continues its row, and copied whole to a free page for every other.  Rows that nothing continues are given up: pages that no
  * table names any more are free, and may be taken by this call's copies.
- *  in, out  of the same table_pages; no array of out overlaps one of in, but uses, which may be the same
+ *  in, out  of the same table_pages; no array of out overlaps one of in, but uses, which may be the same, and none overlaps parents
  * uses may count entries of other tables too; such pages stay.
  */
 int shflbw_kv_fork(const shflbw_kv_cache* cache, const shflbw_kv_pages* in, const shflbw_kv_pages* out, const int32_t* parents,

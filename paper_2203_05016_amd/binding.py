@@ -755,7 +755,7 @@ class KVCache:
 
         Full pages are shared; a last page that is not full is copied to a free one for all but the first that continues its
         row.  Rows that nothing continues give their pages up.  Returns the new (table, lengths, uses); out: their memory, which
-        must not be the arguments' own but for uses."""
+        must not be the arguments' own but for uses, nor that of parents."""
         if stream is None and self._plan is not None:
             r = _calls.kv_fork(self._plan, table, lengths, uses, parents, out)   # None: not the plain case
             if r is not None:

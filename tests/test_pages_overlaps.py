@@ -1,0 +1,47 @@
+"""Memory that a call on pages may not be given twice: its kernels read some arrays again when they have written others, and by what they read they find their
+way in memory.  No GPU: addresses that nothing follows; every call must end before it reaches a launch."""
+import pytest
+
+from paper_2203_05016_amd import binding
+
+BAD_SHAPE = -2
+HERE = 1 << 20
+ROWS, WIDTH, PAGES = 3, 4, 8
+CACHE = binding._Cache(128, PAGES, 32, 2, 64, 0)
+# where the arrays of one side lie, and how many numbers they hold
+ARRAYS = {"table": (0, ROWS * WIDTH), "lengths": (4096, ROWS), "uses": (8192, PAGES)}
+
+
+def side(at, **kw):
+    return binding._Pages(**{**dict(sequences=ROWS, table_pages=WIDTH, table_ld=WIDTH), **{name: at + off for name, (off, _) in ARRAYS.items()}, **kw})
+
+
+def need():
+    return binding.lib().shflbw_kv_pages_workspace(CACHE, ROWS)
+
+
+def extend(i, o, counts=7 * HERE, slots=6 * HERE, starts=5 * HERE, tokens=9, work=8 * HERE):
+    return binding.lib().shflbw_kv_extend(CACHE, i, o, counts, slots, starts, tokens, work, need(), None)
+
+
+def fork(i, o, parents=7 * HERE, work=8 * HERE):
+    return binding.lib().shflbw_kv_fork(CACHE, i, o, parents, work, need(), None)
+
+
+def compact(i, o, work=8 * HERE):
+    return binding.lib().shflbw_kv_compact(CACHE, i, o, work, need(), None)
+
+
+def ends(base, have, size):
+    """Addresses of `size` numbers that share the first or the last of the `have` numbers at base."""
+    return base, base + 4 * (have - 1), base - 4 * (size - 1)
+
+
+@pytest.mark.parametrize("name", ARRAYS)
+def test_results_over_what_is_read_again(name):
+    """The copies of a fork look up their sources by the parents once lengths, table and uses are written."""
+    off, have = ARRAYS[name]
+    for at in ends(2 * HERE + off, have, ROWS):
+        assert fork(side(HERE), side(2 * HERE), parents=at) == BAD_SHAPE, (name, at)
+        assert extend(side(HERE), side(2 * HERE), counts=at) == BAD_SHAPE, (name, at)
+        assert extend(side(2 * HERE), side(2 * HERE), counts=at) == BAD_SHAPE, (name, at)
