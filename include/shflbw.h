@@ -444,6 +444,7 @@ int64_t shflbw_kv_pages_workspace(const shflbw_kv_cache* cache, int sequences);
  *  slots    device, tokens: the slots of the new tokens, sequence after sequence, to be written to; -1 where there is no page, and
  *           past the last token.  Tokens past `tokens` have no slot.
  *  starts   device, sequences + 1: where each sequence's begin (shflbw_kv_sequences.starts of their queries)
+ *           slots and starts overlap no other array of the call.
  * Lengths and starts stop at 2^31 - 1.  A last page that is not yet full must not be shared (shflbw_kv_fork leaves none that is).
  */
 int shflbw_kv_extend(const shflbw_kv_cache* cache, const shflbw_kv_pages* in, const shflbw_kv_pages* out, const int32_t* counts,

@@ -726,7 +726,8 @@ class KVCache:
         table (sequences, pages) int32: the pages of every sequence in order, lengths (sequences,) int32 its tokens, uses (pages of the cache,)
         int32 how many entries of tables name each page; counts (sequences,) int32.  tokens: how many slots are wanted, at least what
         counts add up to.  Returns (table, lengths, uses, slots, starts): slots (tokens,) for ``write``, -1 where there is no page left and past the last token,
-        starts (sequences + 1,) for ``attention``.  out: the first three's memory, which may be the arguments' own; slots, starts: theirs."""
+        starts (sequences + 1,) for ``attention``.  out: the first three's memory, which may be the arguments' own; slots, starts: theirs,
+        which no other array may overlap."""
         if stream is None and self._plan is not None:
             r = _calls.kv_extend(self._plan, table, lengths, uses, counts, tokens, out, slots, starts)   # None: not the plain case
             if r is not None:

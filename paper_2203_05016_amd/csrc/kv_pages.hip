@@ -639,8 +639,9 @@ int check_pages(const shflbw_kv_pages* p)
 }
 // Checks what the three calls have in common and fills in a.  in_place: tables and lengths may be the same.  lengths: they are needed.  which: counts or
 // parents, one for each row of out, if the call has such; kernels read them again when they have written rows of out, so that they may not be part of it.
+// more: what else the call writes.
 int begin(PagesArgs& a, const shflbw_kv_cache* c, const shflbw_kv_pages* in, const shflbw_kv_pages* out, bool in_place, bool lengths, const int32_t* which,
-          void* workspace, int64_t workspace_bytes)
+          const Span (&more)[2], void* workspace, int64_t workspace_bytes)
 {
     int rc = check_cache(c);
     if (rc < 0 || (rc = check_pages(in)) < 0 || (rc = check_pages(out)) < 0) return rc;
@@ -656,8 +657,13 @@ int begin(PagesArgs& a, const shflbw_kv_cache* c, const shflbw_kv_pages* in, con
             if (overlap(to[i], from[j]) && !same) return fail(SHFLBW_ERR_BAD_SHAPE, "arrays of out overlap those of in");
             if (i != j && overlap(to[i], to[j])) return fail(SHFLBW_ERR_BAD_SHAPE, "arrays of out overlap each other");
         }
-    for (int i = 0; which && i < 3; ++i)
-        if (overlap(to[i], {which, out->sequences})) return fail(SHFLBW_ERR_BAD_SHAPE, "arrays of out overlap counts or parents");
+    const Span chosen = {which, which ? out->sequences : 0};
+    for (int i = 0; i < 3; ++i) {
+        if (overlap(to[i], chosen)) return fail(SHFLBW_ERR_BAD_SHAPE, "arrays of out overlap counts or parents");
+        for (const Span& x : more)
+            if (overlap(x, from[i]) || overlap(x, to[i]) || overlap(x, chosen)) return fail(SHFLBW_ERR_BAD_SHAPE, "slots or starts overlap another array");
+    }
+    if (overlap(more[0], more[1])) return fail(SHFLBW_ERR_BAD_SHAPE, "slots and starts overlap");
     const int64_t sequences = in->sequences > out->sequences ? in->sequences : out->sequences;
     if (!workspace || workspace_bytes < workspace_bytes_of(c->pages, sequences))
         return fail(SHFLBW_ERR_NULL_ARG, "the call needs a workspace of %lld bytes", (long long)workspace_bytes_of(c->pages, sequences));
@@ -706,9 +712,9 @@ int shflbw_kv_extend(const shflbw_kv_cache* cache, const shflbw_kv_pages* in, co
 {
     using namespace shflbw;
     PagesArgs a = {};
-    const int rc = begin(a, cache, in, out, true, true, counts, workspace, workspace_bytes);
-    if (rc < 0) return rc;
     if (tokens < 0 || tokens > INT_MAX) return fail(SHFLBW_ERR_BAD_SHAPE, "tokens must be 0 to 2^31 - 1");
+    const int rc = begin(a, cache, in, out, true, true, counts, {{slots, tokens}, {starts, out ? out->sequences + 1LL : 0}}, workspace, workspace_bytes);
+    if (rc < 0) return rc;
     if (!starts || (tokens && !slots) || (a.rows && !counts)) return fail(SHFLBW_ERR_NULL_ARG, "counts, slots and starts must not be NULL");
     a.which = counts;
     a.slots = slots;
@@ -732,7 +738,7 @@ int shflbw_kv_fork(const shflbw_kv_cache* cache, const shflbw_kv_pages* in, cons
 {
     using namespace shflbw;
     PagesArgs a = {};
-    const int rc = begin(a, cache, in, out, false, true, parents, workspace, workspace_bytes);
+    const int rc = begin(a, cache, in, out, false, true, parents, {}, workspace, workspace_bytes);
     if (rc < 0) return rc;
     if (a.rows && !parents) return fail(SHFLBW_ERR_NULL_ARG, "parents must not be NULL");
     a.which = parents;
@@ -760,7 +766,7 @@ int shflbw_kv_compact(const shflbw_kv_cache* cache, const shflbw_kv_pages* in, c
 {
     using namespace shflbw;
     PagesArgs a = {};
-    const int rc = begin(a, cache, in, out, true, false, nullptr, workspace, workspace_bytes);
+    const int rc = begin(a, cache, in, out, true, false, nullptr, {}, workspace, workspace_bytes);
     if (rc < 0) return rc;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int parts = (int)ceil_div(a.page_bytes, COPY_BYTES), table_blocks = (int)few_blocks(ceil_div((int64_t)a.rows * a.width, 256));

@@ -45,3 +45,17 @@ def test_results_over_what_is_read_again(name):
         assert fork(side(HERE), side(2 * HERE), parents=at) == BAD_SHAPE, (name, at)
         assert extend(side(HERE), side(2 * HERE), counts=at) == BAD_SHAPE, (name, at)
         assert extend(side(2 * HERE), side(2 * HERE), counts=at) == BAD_SHAPE, (name, at)
+
+
+@pytest.mark.parametrize("name", ARRAYS)
+def test_slots_and_starts_over_other_arrays(name):
+    off, have = ARRAYS[name]
+    for base in (HERE, 2 * HERE):
+        for kw in ([dict(slots=at) for at in ends(base + off, have, 9)] + [dict(starts=at) for at in ends(base + off, have, ROWS + 1)]):
+            assert extend(side(HERE), side(2 * HERE), **kw) == BAD_SHAPE, (name, kw)
+
+
+def test_slots_and_starts_over_counts_and_each_other():
+    for kw in ([dict(slots=at) for at in ends(7 * HERE, ROWS, 9)] + [dict(starts=at) for at in ends(7 * HERE, ROWS, ROWS + 1)] +
+               [dict(slots=at) for at in ends(5 * HERE, ROWS + 1, 9)]):
+        assert extend(side(HERE), side(2 * HERE), **kw) == BAD_SHAPE, kw
