@@ -434,7 +434,7 @@ typedef struct {
     int32_t *table, *lengths, *uses;
 } shflbw_kv_pages;
 
-/* Bytes of device workspace that the three calls below need, or a negative status. */
+/* Bytes of device workspace that the three calls below need, or a negative status.  No array of a call overlaps its workspace or the cache. */
 int64_t shflbw_kv_pages_workspace(const shflbw_kv_cache* cache, int sequences);
 
 /*

@@ -664,10 +664,17 @@ int begin(PagesArgs& a, const shflbw_kv_cache* c, const shflbw_kv_pages* in, con
             if (overlap(x, from[i]) || overlap(x, to[i]) || overlap(x, chosen)) return fail(SHFLBW_ERR_BAD_SHAPE, "slots or starts overlap another array");
     }
     if (overlap(more[0], more[1])) return fail(SHFLBW_ERR_BAD_SHAPE, "slots and starts overlap");
-    const int64_t sequences = in->sequences > out->sequences ? in->sequences : out->sequences;
-    if (!workspace || workspace_bytes < workspace_bytes_of(c->pages, sequences))
-        return fail(SHFLBW_ERR_NULL_ARG, "the call needs a workspace of %lld bytes", (long long)workspace_bytes_of(c->pages, sequences));
+    const int64_t sequences = in->sequences > out->sequences ? in->sequences : out->sequences, work = workspace_bytes_of(c->pages, sequences);
+    if (!workspace || workspace_bytes < work) return fail(SHFLBW_ERR_NULL_ARG, "the call needs a workspace of %lld bytes", (long long)work);
     if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(SHFLBW_ERR_BAD_SHAPE, "the workspace must be 16-byte aligned");
+    const int64_t page_bytes = page_head_bytes(c->page_tokens, c->head_dim) * c->heads;
+    const Span own[2] = {{workspace, work / 4}, {c->data, c->pages * page_bytes / 4}};
+    if (overlap(own[0], own[1])) return fail(SHFLBW_ERR_BAD_SHAPE, "the workspace overlaps the cache");
+    for (const Span& x : own) {
+        bool any = overlap(x, chosen) || overlap(x, more[0]) || overlap(x, more[1]);
+        for (int i = 0; i < 3; ++i) any |= overlap(x, from[i]) || overlap(x, to[i]);
+        if (any) return fail(SHFLBW_ERR_BAD_SHAPE, "an array overlaps the workspace or the cache");
+    }
     a.table_in = in->table;
     a.table_out = out->table;
     a.lengths_in = in->lengths;
@@ -683,7 +690,7 @@ int begin(PagesArgs& a, const shflbw_kv_cache* c, const shflbw_kv_pages* in, con
     a.page_shift = __builtin_ctz(c->page_tokens);
     a.page_blocks = (int)ceil_div(c->pages, PAGES_BLOCK);
     a.data = static_cast<char*>(c->data);
-    a.page_bytes = page_head_bytes(c->page_tokens, c->head_dim) * c->heads;
+    a.page_bytes = page_bytes;
     carve(a, workspace, sequences);
     return SHFLBW_OK;
 }

@@ -59,3 +59,25 @@ def test_slots_and_starts_over_counts_and_each_other():
     for kw in ([dict(slots=at) for at in ends(7 * HERE, ROWS, 9)] + [dict(starts=at) for at in ends(7 * HERE, ROWS, ROWS + 1)] +
                [dict(slots=at) for at in ends(5 * HERE, ROWS + 1, 9)]):
         assert extend(side(HERE), side(2 * HERE), **kw) == BAD_SHAPE, kw
+
+
+def test_workspace_and_cache_over_arrays():
+    """What lies in the workspace is an array's place there: lists of pages, ranks, counts.  The cache's bytes are 128 to 128 + 8 pages of 4352."""
+    size = need() // 4
+    arrays = [(base + off, have) for base in (HERE, 2 * HERE) for off, have in ARRAYS.values()]
+    for at, have in arrays:
+        # (multiples of 16, as the workspace has to be)
+        for work in (at, at + 4 * (have - 1) & ~15, (at - 4 * (size - 1) + 15) & ~15):
+            for call in (extend, fork, compact):
+                if call is not compact or at not in (HERE + 4096, 2 * HERE + 4096):          # which has no lengths
+                    assert call(side(HERE), side(2 * HERE), work=work) == BAD_SHAPE, (call, hex(at), hex(work))
+    for at in (7 * HERE, 6 * HERE, 5 * HERE):
+        assert extend(side(HERE), side(2 * HERE), work=at) == BAD_SHAPE
+    assert fork(side(HERE), side(2 * HERE), parents=8 * HERE) == BAD_SHAPE
+    inside = 128 + 8 * 4352 - 4
+    for name in ARRAYS:
+        for call in (extend, fork, compact):
+            if call is not compact or name != "lengths":
+                assert call(side(HERE, **{name: inside}), side(2 * HERE)) == BAD_SHAPE and call(side(HERE), side(2 * HERE, **{name: inside})) == BAD_SHAPE
+    assert fork(side(HERE), side(2 * HERE), parents=inside) == BAD_SHAPE and extend(side(HERE), side(2 * HERE), slots=inside) == BAD_SHAPE
+    assert compact(side(HERE), side(2 * HERE), work=1024) == BAD_SHAPE
