@@ -798,8 +798,8 @@ def norm_rotate(q, k, head_dim, positions, frequencies, axes=None, q_weight=None
     of its mean square (plus eps), times weights (head_dim,), then turned by its position.  norm False: only turned.
 
     frequencies (pairs,) float64: radians per step of the position for each pair of features, i and i + pairs (interleaved: 2 i and 2 i + 1); the
-    features past 2 * pairs are not turned.  positions (tokens,) or (rows, tokens) int32; axes (pairs,) int32: which row each pair goes by, the first
-    without it.  All on the GPU.  Returns (q, k) of q's dtype; q_out, k_out: their memory, which may be q and k themselves."""
+    features past 2 * pairs are not turned.  positions (tokens,) or (rows, tokens) int32 (None where there are no frequencies: norms alone);
+    axes (pairs,) int32: which row each pair goes by, the first without it.  All on the GPU.  Returns (q, k) of q's dtype; q_out, k_out: their memory, which may be q and k themselves."""
     if stream is None and (_calls or calls()):
         r = _calls.norm_rotate(q, k, head_dim, positions, frequencies, axes, q_weight, k_weight, eps, norm, interleaved, q_out, k_out)
         if r is not None:                       # None: not the plain case, all checks below
@@ -821,10 +821,13 @@ def norm_rotate(q, k, head_dim, positions, frequencies, axes=None, q_weight=None
     pairs = frequencies.shape[0]
     if 2 * pairs > head_dim:
         raise ValueError("%d frequencies for heads of %d features" % (pairs, head_dim))
-    if positions.dtype != torch.int32 or positions.dim() not in (1, 2) or positions.shape[-1] != tokens or (tokens > 1 and positions.stride(-1) != 1):
+    if positions is None and pairs:
+        raise ValueError("%d frequencies without positions" % pairs)
+    if positions is not None and (positions.dtype != torch.int32 or positions.dim() not in (1, 2) or positions.shape[-1] != tokens or
+                                  (tokens > 1 and positions.stride(-1) != 1)):
         raise TypeError("positions must be int32, (%d,) or (rows, %d), with unit token stride" % (tokens, tokens))
-    position_rows = positions.shape[0] if positions.dim() == 2 else 1
-    ldp = positions.stride(0) if positions.dim() == 2 and position_rows > 1 else max(tokens, 1)
+    position_rows = positions.shape[0] if positions is not None and positions.dim() == 2 else 1
+    ldp = positions.stride(0) if position_rows > 1 else max(tokens, 1)
     if ldp < tokens:
         raise ValueError("rows of positions overlap")
     if position_rows < 1:
@@ -854,7 +857,7 @@ def norm_rotate(q, k, head_dim, positions, frequencies, axes=None, q_weight=None
     r = _Rotation(head_dim, BF16 if q.dtype == torch.bfloat16 else F16, pairs, bool(interleaved), bool(norm), position_rows, float(eps),
                   frequencies.data_ptr(), address(axes), address(q_weight), address(k_weight))
     with on:
-        _check(lib().shflbw_norm_rotate(r, positions.data_ptr(), ldp, q.data_ptr(), ldq, q_rows // head_dim, address(k), ldk, k_rows // head_dim,
+        _check(lib().shflbw_norm_rotate(r, address(positions), ldp, q.data_ptr(), ldq, q_rows // head_dim, address(k), ldk, k_rows // head_dim,
                                         q_out.data_ptr(), ldqo, address(k_out), ldko, tokens, handle))
     return q_out, k_out
 
