@@ -410,7 +410,7 @@ int64_t shflbw_kv_shared_attention_workspace(const shflbw_kv_cache* cache, const
  * Attention over the cache of sequences that share prefixes: every query sees all tokens of its sequence's prefix, and its
  * sequence's own tokens up to its own position, as in shflbw_kv_attention, whose table, lengths and
  * positions are the own tokens' alone (a length of 0, or below the queries, leaves queries with the prefix).  A long prefix is read
- * from memory once for all its sequences.  window must be 0 (under a window a far prefix is not seen: shflbw_kv_attention takes its pages
+ * from memory once for all its sequences, but where most of them have 20 queries or more: it is then read for every 32 of these.  window must be 0 (under a window a far prefix is not seen: shflbw_kv_attention takes its pages
  * in the sequence's table).  Columns of q before the first sequence's and behind the last one's are left as they were.
  * Everything else, the workspace and accuracy included, is as in shflbw_kv_attention.
  */

@@ -73,6 +73,15 @@ AttnPlan plan_prefix(int64_t pairs, int group, int D, int64_t max_sharing, int64
     return p;
 }
 
+// Items of 32 queries of a head that `tokens` queries of `batch` sequences may be more than they would be in sequences of max_queries (2 or more) each: at most so
+// many have max_queries that every other still has one
+double uneven_items(int64_t batch, int64_t tokens, int64_t max_queries)
+{
+    const int64_t sequences = std::min(batch, tokens), items = ceil_div(max_queries, ATTN_TILE_QUERIES);
+    const int64_t whole = std::min((tokens - sequences) / (max_queries - 1), sequences);
+    return (double)(whole * items + sequences - whole) - (double)tokens / (double)max_queries * (double)items;
+}
+
 }  // namespace
 
 AttnPlan plan_cache_attention(int batch, int heads, int group, int D, int64_t tokens, int max_queries, int64_t max_length, int window, int sinks)
@@ -122,12 +131,18 @@ SharedPlan plan_shared_attention(int prefixes, int64_t max_sharing, int64_t max_
     const auto parts = [&](int64_t n) { return product(n * (D + 2) * 4, (int64_t)heads * group * tokens); };
     // From 20 queries on, sequence by sequence: a prefix's parts, in 32 bits, are then more than its keys.  32 sequences behind 4096 tokens, 64 heads over 8 of
     // 128: 16 queries 137 us, prefix and own apart 116; 20 131 and 151, 32 129 and 180, 33 240 and 292; 8 of 512 504 and 752.
+    // Sequences of few queries among those of many are items of 32 columns there that read their prefix for a few: not where, for all that the host knows (every sequence
+    // has a query, and as many as can have the most), such items are so many that their keys come to over 75 for each column of q.  With prefix
+    // and own apart, then without, 64 heads over 8 of 128, one prefix of 8001 tokens: 63 sequences of 1 query and one of 512 (849 keys a column) 375 us and 1910, 56 and
+    // 8 of 512 (104) 1521 and 2359, 15 and one of 512 (220) 285 and 631; behind 1000 tokens 63 and one (106) 204 and 362, but 56 and 8 (13) 577 and 468; behind 200, 60 and
+    // 4 of 200 (14) 120 and 89; 32 over 8 of 96 behind 4096, 31 and one of 1024 (116) 215 and 518.  What the
+    // host does not know costs less: if the 56 others have none 1233 and 988; 32 of 10 and 32 of 30 queries (133) 525 and 480.
     // And few queries where reading the prefix again for every sequence, from the L2s, is less than parts and another launch: up to 2^27 values (bytes, as
     // the cache has them, are 17/32 of that).  64 heads over 8 of 128: 8 sequences behind 500 tokens 8.5 us and 18.8 apart, 32 behind 1000 12.0 and 22.7, behind 2000
     // (131 million) 20.7 and 23.6; 32 over 8 of 96, 8 prefixes of 3000 with 4 each (147 million) 20.2 and 18.0.
-    const bool many = max_queries >= 20;
+    const bool many = max_queries >= 20 && uneven_items(batch, tokens, max_queries) * (double)max_prefix <= 75.0 * (double)tokens;
     const int64_t again = product((int64_t)batch * heads * 2 * D, max_prefix);
-    p.behind = keys_fit && (many || ((int64_t)group * max_queries <= 64 && again <= 1LL << 27));
+    p.behind = keys_fit && (many || (max_queries < 20 && (int64_t)group * max_queries <= 64 && again <= 1LL << 27));
     if (p.behind) {
         const int64_t keys = max_prefix + ATTN_TILE_KEYS + max_length;
         p.own = many ? plan_tiles((int64_t)batch * heads, ceil_div(max_queries, ATTN_TILE_QUERIES) * group, D, keys)

@@ -66,4 +66,12 @@ CASES = [
     Case("tiles, one part", 32, 2, 64, "f16", [2, 1], [90, 33], [70, 9, 150], [9, 10, 17], plan=dict(behind=0, joins=0, own=tiles(splits=1))),
     Case("tiles, several parts", 32, 2, 128, "bf16", [2, 1], [200, 33], [700, 9, 900], [9, 10, 17], plan=dict(behind=0, joins=0, own=tiles())),
     Case("tiles, heads of 96", 18, 1, 96, "f16", [1, 1, 1], [64, 0, 31], [5, 700, 64], [9, 19, 12], plan=dict(behind=0, joins=0, own=tiles())),
+    # a part of a prompt among single tokens: the prefix once for all columns, if it is long; prompts and shorter ones, which are much alike
+    Case("one of 70 among single tokens", 8, 2, 64, "f16", [12], [150], _spread(12, 1, 90), [1] * 5 + [70] + [1] * 6, most=4000,
+         plan=dict(behind=0, joins=0, prefix=tiles(), own=tiles())),
+    Case("one of 70 among single tokens, of three prefixes", 10, 2, 128, "bf16", [4, 0, 8], [70, 9, 100], _spread(12, 1, 90), [1, 0, 1, 70] + [1] * 6 + [0, 3], most=3000,
+         plan=dict(behind=0, prefix=tiles())),
+    Case("one of 70 among single tokens behind a short prefix", 8, 2, 64, "bf16", [12], [150], _spread(12, 1, 90), [1] * 5 + [70] + [1] * 6,
+         plan=dict(behind=1, own=tiles())),
+    Case("prompts of 20 to 40", 4, 2, 96, "f16", [2, 3], [150, 90], _spread(5, 1, 90), [20, 40, 33, 30, 31], most=2000, plan=dict(behind=1, own=tiles(4))),
 ]
