@@ -646,7 +646,7 @@ class KVCache:
         int32: the prefixes' pages and tokens.  members (prefixes + 1,) int32: prefix g is that of sequences ``members[g]`` to
         ``members[g + 1] - 1``; without members one prefix is everybody's.  max_prefix: the longest prefix's tokens (all of the table's pages by
         default), which decides how the work is cut only.  max_sharing: at least the columns of q that any prefix's sequences have
-        together (all of them by default)."""
+        together (all of them by default); columns past it, and those of sequences of no prefix, are left undefined."""
         if stream is None and self._plan is not None:
             r = _calls.shared_attention(self._plan, q, prefix_table, prefix_lengths, table, lengths, members, starts, max_queries, max_length, max_prefix,
                                         max_sharing, out)   # None: not the plain case, all checks below

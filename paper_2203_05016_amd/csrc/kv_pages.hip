@@ -5,7 +5,8 @@
 //
 // Bound by latency (a launch for every step that needs all of the step before, 3 to 5 us each on the GPU, of which most is the chain of loads and barriers) but
 // for the pages that are copied.  64 sequences, one token more, 8192 pages: 7.7 us; 256 prompts of up to 8192 tokens, 65536 pages: 15.4; 512 sequences continued by
-// 8 each, 16000 pages, 15 MB copied: 17; 2000 of 8000 pages of 70 KB to the front: 51 us, 5.4 TB/s (a large copy 5.2).
+// 8 each, 16000 pages, 15 MB copied: 17; 2000 of 8000 pages of 70 KB to the front: 51 us, 5.4 TB/s, where part of it lies in
+// the memory-side cache, 65, 4.3 TB/s, where nothing does (a large copy 5.2).
 #include <hip/hip_runtime.h>
 
 #include <climits>

@@ -147,7 +147,8 @@ __device__ __forceinline__ void rot_tables(const RotateArgs& a, int64_t token0, 
     }
     __syncthreads();
 }
-// whether a sum of squares in 32 bits can be relied on
+// Whether a sum of squares in 32 bits can be relied on, whatever eps is.  A column of zeros is not ordinary by this, and in the kernel for many tokens the 32 or 64
+// tokens of its wavefront go token by token: 72 heads of 128 by 8192 56 us, 209 if the last 5 columns are zeros, 706 if one in 32 is; by 64 tokens 5.8 whatever there is.
 __device__ __forceinline__ bool rot_ordinary(float sum) { return sum > 0x1p-60f && sum < 0x1p120f; }
 template <int D>
 __device__ __forceinline__ float rot_root(float sum, float eps) { return __builtin_amdgcn_rsqf(sum * (1.0f / D) + eps); }
